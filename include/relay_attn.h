@@ -465,6 +465,114 @@ ra_status relay_attn_system_fill(const ra_params *p,
                                  void *hip_stream);
 
 /*
+ * A context cache in 4 bits.  Same paging as the bf16 cache; a block of one kv head holds
+ *   codes    [block_size][head_dim / 2] bytes, channel 2i of a position in the low half of byte i, 2i + 1 in the high
+ *            half; a half is a sign (8) and one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 .. 7)
+ *   scales   [head_dim / 32][block_size] bytes behind them: 32 consecutive channels of a position share the power of two
+ *            2^(byte - 127); bytes 0 .. 252
+ * so k_cache and v_cache are [num_blocks][num_kv_heads][block_size * (head_dim / 2 + head_dim / 32)] bytes: 17/64 of the
+ * bf16 cache.  A value is its magnitude times its block's power of two; attention takes it as that, exactly (in
+ * bf16 products with fp32 sums), so the result is that of the bf16 entry points on the same values.  The shared
+ * system cache stays bf16: it is read once per batch, and stored once.
+ *   block_size is a power of two from 8 on here (RA_ERR_UNSUPPORTED below).  Positions at or beyond a request's length
+ * that share its last block may be read, whatever they hold, and count for nothing; block-table slots behind the ones in use
+ * are never followed.
+ * relay_attn_fp4_cache_bytes: host arithmetic; the bytes of one (block, kv head) and of one whole cache (k or v) for
+ * p->num_blocks, num_kv_heads, block_size and head_dim.
+ */
+ra_status relay_attn_fp4_cache_bytes(const ra_params *p, size_t *block_bytes_out, size_t *bytes_out);
+
+/*
+ * relay_attn_cache_append for the 4-bit cache: rounds the new keys/values into it.  For each 32 channels of a row, a
+ * being the largest magnitude, the power of two is 2^(floor(log2 a) - 2), twice that where a >= 1.75 * 2^floor(log2 a), and within
+ * 2^-127 .. 2^125; values round to the nearest multiple there (halves to the even code) and saturate at 6.  So no finite value below
+ * 2^127 is off by more than half a step of the grid, 1/6 of itself or 1/14 of a.  The format has no infinity and no NaN: both count
+ * as the largest magnitude and are stored as 6 * 2^125, so that a row with one in it spoils every result that sees it and no other.
+ *   slot_map       NULL: new token j of request i goes to the position that relay_attn_cache_append gives it.  Otherwise
+ *                  device, [total_q]: the place of each token, physical block * block_size + offset in it
+ *                  (relay_attn_update_tables writes such a map); a token whose entry is not in 0 .. num_blocks *
+ *                  block_size - 1 is left out.  cu_seqlens_q, block_tables and context_lens are not read then and may be
+ *                  NULL.  Entries in range must differ.
+ * Only the bytes of the rows named are written.
+ */
+ra_status relay_attn_cache_append_fp4(const ra_params *p,
+                                      const void *k_new, const void *v_new,
+                                      int64_t new_stride_token, int64_t new_stride_head,
+                                      const int32_t *cu_seqlens_q, int32_t total_q,
+                                      const int32_t *slot_map,
+                                      void *k_cache, void *v_cache,
+                                      const int32_t *block_tables, const int32_t *context_lens,
+                                      void *hip_stream);
+
+/*
+ * The way back: the values of rows of the 4-bit cache as bf16 (exact), named as in relay_attn_cache_append_fp4, into
+ * k_out / v_out, [total_q] tokens x Hkv x head_dim addressed by the strides given.  With the strides of a system cache it
+ * turns a request's context (m_i = context_lens[i] "new" tokens) into a shared system prompt.  Rows whose slot is out of
+ * range are left as they are.
+ */
+ra_status relay_attn_cache_read_fp4(const ra_params *p,
+                                    void *k_out, void *v_out,
+                                    int64_t out_stride_token, int64_t out_stride_head,
+                                    const int32_t *cu_seqlens_q, int32_t total_q,
+                                    const int32_t *slot_map,
+                                    const void *k_cache, const void *v_cache,
+                                    const int32_t *block_tables, const int32_t *context_lens,
+                                    void *hip_stream);
+
+/*
+ * relay_attn_decode and relay_attn_prefill over a 4-bit context cache: arguments, result, workspace and errors as there.
+ */
+ra_status relay_attn_decode_fp4(const ra_params *p,
+                                const void *q,
+                                const void *k_sys, const void *v_sys,
+                                const void *k_cache, const void *v_cache,
+                                const int32_t *block_tables, const int32_t *context_lens,
+                                void *out, float *lse_out,
+                                void *workspace, size_t workspace_bytes,
+                                void *hip_stream);
+
+ra_status relay_attn_prefill_fp4(const ra_params *p,
+                                 const void *q,
+                                 const int32_t *cu_seqlens_q, int32_t total_q, int32_t max_q_len,
+                                 const void *k_sys, const void *v_sys,
+                                 const void *k_cache, const void *v_cache,
+                                 const int32_t *block_tables, const int32_t *context_lens,
+                                 void *out, float *lse_out,
+                                 void *workspace, size_t workspace_bytes,
+                                 void *hip_stream);
+
+/*
+ * Block tables of a scheduler step, built on the device from request lengths, for either kind of cache: blocks for
+ * requests that grow, blocks back from requests that shrink (drafted tokens taken back) or end (new length 0), and what the
+ * step's other calls want: lengths, cu_seqlens_q and the slots of the new tokens.
+ *   old_lens, new_lens  [batch] lengths before and behind the step; a negative one counts as 0.  Row i of block_tables
+ *                  holds ceil(old_lens[i] / block_size) blocks (old lengths are cut off at the row's capacity).
+ *   pool_in        [2]: [0] = height of the stack of free blocks
+ *   free_blocks    [num_blocks] the stack, its free block ids at 0 .. height - 1; updated
+ *   block_tables   [batch][max_blocks_per_seq]; updated: columns that come into use are written, the others left
+ *   pool_out       [2], another array than pool_in: [0] = the new height, [1] = number of requests not served
+ *   context_lens   [batch], another array than the lengths: new_lens[i], or old_lens[i] where request i is not served
+ *   cu_seqlens_q   nullable; [batch + 1]: running sums of max(0, new_lens[i] - old_lens[i]), served or not, so that they fit
+ *                  the packed new tokens of the caller
+ *   slot_map       [num_slots] (may be NULL if that is 0): for each packed new token physical block * block_size + offset;
+ *                  -1 for tokens of requests that are not served, and behind the last token
+ * Blocks that come back go on top of the stack in (request, column) order; then requests take theirs from the top in that
+ * order.  A request that needs blocks is served as long as the stack holds what it and all requests in front of it
+ * ask for; one that needs none always is, and one whose new length exceeds max_blocks_per_seq * block_size never.  The same call on the same
+ * inputs has the same results, and may be repeated on its own outputs (the inputs that it updates are
+ * still good for it).
+ * Uses p->batch, block_size, num_blocks and max_blocks_per_seq only.  block_tables entries and stack entries are
+ * taken on trust as in every call (an id out of range gets its tokens the slot -1).  RA_ERR_UNSUPPORTED where num_blocks *
+ * block_size, or batch * max_blocks_per_seq + num_blocks, exceeds 31 bits.
+ */
+ra_status relay_attn_update_tables(const ra_params *p,
+                                   const int32_t *old_lens, const int32_t *new_lens,
+                                   const int32_t *pool_in, int32_t *pool_out, int32_t *free_blocks,
+                                   int32_t *block_tables, int32_t *context_lens,
+                                   int32_t *cu_seqlens_q, int32_t *slot_map, int32_t num_slots,
+                                   void *hip_stream);
+
+/*
  * Debug aid: checks on the device what the attention entry points take on trust, the CONTENTS
  * of the index arrays (Alg. 1 indexes the cache with them: an entry out of range is a read
  * out of bounds).  Unlike every other entry point it SYNCHRONISES the stream and copies 16

@@ -26,6 +26,8 @@ EXPORTED = ("relay_attn_workspace_bytes", "relay_attn_decode_plan", "relay_attn_
             "relay_attn_decode_static", "relay_attn_static_scratch_bytes",
             "relay_attn_decode_grouped", "relay_attn_group_requests", "relay_attn_prefill_multi",
             "relay_attn_debug_stream_probe", "relay_attn_debug_launch_probe",
+            "relay_attn_fp4_cache_bytes", "relay_attn_cache_append_fp4", "relay_attn_cache_read_fp4",
+            "relay_attn_decode_fp4", "relay_attn_prefill_fp4", "relay_attn_update_tables",
             "relay_attn_status_string", "relay_attn_abi_version")
 
 
@@ -126,6 +128,17 @@ def load() -> ctypes.CDLL:
     lib.relay_attn_prefill.argtypes = [P, V, V, I32, I32, V, V, V, V, V, V, V, V, V, SZ, V]
     lib.paged_attn_decode_naive.restype = ctypes.c_int
     lib.paged_attn_decode_naive.argtypes = [P, V, V, V, V, V, V, V, V, SZ, V]
+    lib.relay_attn_fp4_cache_bytes.restype = ctypes.c_int
+    lib.relay_attn_fp4_cache_bytes.argtypes = [P, ctypes.POINTER(SZ), ctypes.POINTER(SZ)]
+    for fn in (lib.relay_attn_cache_append_fp4, lib.relay_attn_cache_read_fp4):
+        fn.restype = ctypes.c_int
+        fn.argtypes = [P, V, V, ctypes.c_int64, ctypes.c_int64, V, I32, V, V, V, V, V, V]
+    lib.relay_attn_decode_fp4.restype = ctypes.c_int
+    lib.relay_attn_decode_fp4.argtypes = lib.relay_attn_decode.argtypes
+    lib.relay_attn_prefill_fp4.restype = ctypes.c_int
+    lib.relay_attn_prefill_fp4.argtypes = lib.relay_attn_prefill.argtypes
+    lib.relay_attn_update_tables.restype = ctypes.c_int
+    lib.relay_attn_update_tables.argtypes = [P, V, V, V, V, V, V, V, V, V, I32, V]
     lib.relay_attn_cache_append.restype = ctypes.c_int
     lib.relay_attn_cache_append.argtypes = [P, V, V, ctypes.c_int64, ctypes.c_int64, V, I32, V, V, V, V, V]
     lib.relay_attn_debug_validate.restype = ctypes.c_int
@@ -165,7 +178,8 @@ def _stream():
 def make_params(q, out, k_sys, k_cache, block_tables, *, batch, softmax_scale,
                 max_context_len=0, sys_chunk_tokens=0, ctx_part_tokens=0) -> RAParams:
     """Fill ra_params from tensor shapes/strides.  q/out: [tokens, Hq, d]; k_sys: [s, Hkv, d]
-    (any token/head strides) or None; k_cache: [num_blocks, Hkv, block_size, d] contiguous."""
+    (any token/head strides) or None; k_cache: [num_blocks, Hkv, block_size, d] contiguous, or a 4-bit
+    one, uint8 of the shape that fp4_cache_shape gives."""
     import torch
     p = RAParams()
     p.batch = int(batch)
@@ -173,6 +187,9 @@ def make_params(q, out, k_sys, k_cache, block_tables, *, batch, softmax_scale,
     p.num_kv_heads = int(k_cache.shape[1])
     p.sys_len = 0 if k_sys is None else int(k_sys.shape[0])
     p.block_size = int(k_cache.shape[2])
+    if k_cache.dtype == torch.uint8:                   # head_dim * 17 / 32 bytes a position
+        assert k_cache.dim() == 3 and k_cache.shape[2] * 32 % (17 * p.head_dim) == 0
+        p.block_size = int(k_cache.shape[2]) * 32 // (17 * p.head_dim)
     p.num_blocks = int(k_cache.shape[0])
     p.max_blocks_per_seq = int(block_tables.shape[1])
     p.max_context_len = int(max_context_len)
@@ -396,3 +413,74 @@ def relay_attn_system_fill(params, k_new, v_new, first_pos, k_sys, v_sys):
         ctypes.byref(params), _ptr(k_new), _ptr(v_new), int(k_new.stride(0)), int(k_new.stride(1)),
         int(first_pos), int(k_new.shape[0]), _ptr(k_sys), _ptr(v_sys), _stream())
     _check(st, "relay_attn_system_fill")
+
+
+# ---- the context cache in 4 bits, and block tables built on the device ------------------------------------------
+
+def fp4_cache_shape(num_blocks, num_kv_heads, block_size, head_dim):
+    """Shape of a 4-bit k or v cache (uint8, contiguous): [num_blocks, Hkv, bytes of a block]."""
+    p = RAParams()
+    p.num_blocks, p.num_kv_heads, p.block_size, p.head_dim = int(num_blocks), int(num_kv_heads), int(block_size), int(head_dim)
+    block, total = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().relay_attn_fp4_cache_bytes(ctypes.byref(p), ctypes.byref(block), ctypes.byref(total)),
+           "relay_attn_fp4_cache_bytes")
+    return int(num_blocks), int(num_kv_heads), block.value
+
+
+def _fp4_rows(fn, where, params, k, v, cu_seqlens_q, total_q, k_cache, v_cache, block_tables, context_lens, slot_map):
+    assert k.stride() == v.stride() and k.stride(2) == 1
+    _check(fn(ctypes.byref(params), _ptr(k), _ptr(v), int(k.stride(0)), int(k.stride(1)), _ptr(cu_seqlens_q),
+              int(total_q), _ptr(slot_map), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(context_lens),
+              _stream()), where)
+
+
+def relay_attn_cache_append_fp4(params, k_new, v_new, cu_seqlens_q, total_q, k_cache, v_cache, block_tables,
+                                context_lens, slot_map=None):
+    """k_new / v_new: [total_q, Hkv, d] tensors (any token / head strides, d contiguous), rounded into the 4-bit caches;
+    slot_map: int32 [total_q], or None for the places that lengths and tables give."""
+    _fp4_rows(load().relay_attn_cache_append_fp4, "relay_attn_cache_append_fp4", params, k_new, v_new, cu_seqlens_q,
+              total_q, k_cache, v_cache, block_tables, context_lens, slot_map)
+
+
+def relay_attn_cache_read_fp4(params, k_out, v_out, cu_seqlens_q, total_q, k_cache, v_cache, block_tables, context_lens,
+                              slot_map=None):
+    """k_out / v_out: bf16 [total_q, Hkv, d] tensors (any token / head strides, d contiguous) that take the values of the
+    rows named as in relay_attn_cache_append_fp4."""
+    _fp4_rows(load().relay_attn_cache_read_fp4, "relay_attn_cache_read_fp4", params, k_out, v_out, cu_seqlens_q,
+              total_q, k_cache, v_cache, block_tables, context_lens, slot_map)
+
+
+def relay_attn_decode_fp4(params, q, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out, lse_out, workspace):
+    st = load().relay_attn_decode_fp4(
+        ctypes.byref(params), _ptr(q), _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache),
+        _ptr(block_tables), _ptr(context_lens), _ptr(out), _ptr(lse_out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "relay_attn_decode_fp4")
+
+
+def relay_attn_prefill_fp4(params, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables,
+                           context_lens, out, lse_out, workspace):
+    st = load().relay_attn_prefill_fp4(
+        ctypes.byref(params), _ptr(q), _ptr(cu_seqlens_q), int(total_q), int(max_q_len),
+        _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
+        _ptr(context_lens), _ptr(out), _ptr(lse_out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "relay_attn_prefill_fp4")
+
+
+def make_table_params(block_tables, *, num_blocks, block_size) -> RAParams:
+    """What relay_attn_update_tables reads of ra_params; block_tables: int32 [batch, max_blocks_per_seq]."""
+    p = RAParams()
+    p.batch, p.max_blocks_per_seq = int(block_tables.shape[0]), int(block_tables.shape[1])
+    p.num_blocks, p.block_size = int(num_blocks), int(block_size)
+    return p
+
+
+def relay_attn_update_tables(params, old_lens, new_lens, pool_in, pool_out, free_blocks, block_tables, context_lens,
+                             cu_seqlens_q, slot_map):
+    """int32 device tensors; cu_seqlens_q and slot_map may be None."""
+    st = load().relay_attn_update_tables(
+        ctypes.byref(params), _ptr(old_lens), _ptr(new_lens), _ptr(pool_in), _ptr(pool_out), _ptr(free_blocks),
+        _ptr(block_tables), _ptr(context_lens), _ptr(cu_seqlens_q), _ptr(slot_map),
+        0 if slot_map is None else slot_map.numel(), _stream())
+    _check(st, "relay_attn_update_tables")

@@ -7,6 +7,7 @@
 // internally and converted to natural log only for lse_out.
 #include "ra_device.h"
 #include "ra_kernels.h"
+#include "token_place.h"
 
 namespace ra {
 
@@ -186,34 +187,8 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs
     if (threadIdx.x < kWave) {
         const int lane = (int)threadIdx.x;
         const int token = token0 + lane;
-        // The lanes hold the bounds and lengths of 64 requests at a time, so that a token's place is one trip
-        // to its block id away once they are here (searched first and asked for then, the lengths were a
-        // trip of their own).
-        int req = token, pos = 0;
-        if (a.cu_seqlens_q) {
-            bool found = false;
-            req = a.batch - 1;
-            for (int base = 0; base < a.batch; base += kWave) {
-                const int r = base + lane;
-                const bool any = r < a.batch;
-                const int first = any ? a.cu_seqlens_q[r] : 0, end = any ? a.cu_seqlens_q[r + 1] : INT_MAX;
-                const int len = any ? a.context_lens[r] : 0;
-                int owner = kWave;                        // requests of these that end at or before the token
-                for (int t = 0; t < tpw; ++t) {
-                    const int ended = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= token0 + t));
-                    if (lane == t) owner = ended;
-                }
-                // (a token that no request owns goes to the last one)
-                const bool last = base + kWave >= a.batch;
-                const int from = min(owner, min(a.batch - base, kWave) - 1);
-                const int f = __shfl(first, from), e = __shfl(end, from), l = __shfl(len, from);
-                if (!found && (owner < kWave || last)) {
-                    found = true;
-                    req = base + from;
-                    pos = l - (e - f) + (token - f);
-                }
-            }
-        }
+        int req, pos;
+        place_of_token(a.cu_seqlens_q, a.context_lens, a.batch, token0, tpw, lane, req, pos);
         if (lane < tpw && token < a.total_q) {
             if (!a.cu_seqlens_q) pos = a.context_lens[req] - 1;
             int64_t dst = -1;                             // malformed lengths: write nothing

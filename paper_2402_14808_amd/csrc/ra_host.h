@@ -1,0 +1,39 @@
+// What the host entry points share: the checks of ra_params.
+#pragma once
+#include "../../include/relay_attn.h"
+
+#include <stdint.h>
+
+namespace ra {
+
+constexpr int kFp4LeastBlock = 8;     // the 4-bit kernels take eight positions of a block at a time
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+inline ra_status check_params(const ra_params *p, int32_t total_q) {
+    if (!p) return RA_ERR_INVALID_ARG;
+    if (p->batch < 0 || total_q < 0 || p->num_q_heads < 1 || p->num_kv_heads < 1 ||
+        p->sys_len < 0 || p->block_size < 1 || p->num_blocks < 0 || p->max_blocks_per_seq < 0 ||
+        p->max_context_len < 0 || p->sys_chunk_tokens < 0 || p->ctx_part_tokens < 0 ||
+        p->reserved0 != 0)
+        return RA_ERR_INVALID_ARG;
+    if (p->num_q_heads % p->num_kv_heads != 0) return RA_ERR_INVALID_ARG;
+    if ((p->block_size & (p->block_size - 1)) != 0) return RA_ERR_INVALID_ARG;
+    if (!(p->softmax_scale == p->softmax_scale)) return RA_ERR_INVALID_ARG;  // NaN
+    if (p->out_is_fp32 != 0 && p->out_is_fp32 != 1) return RA_ERR_INVALID_ARG;
+    const int64_t strides[] = {p->q_stride_token, p->q_stride_head, p->o_stride_token,
+                               p->o_stride_head, p->sys_stride_token, p->sys_stride_head};
+    for (int64_t s : strides)
+        if (s < 0 || (s % 8) != 0) return RA_ERR_INVALID_ARG;
+    if (p->sys_chunk_tokens % 32 != 0 || p->ctx_part_tokens % 128 != 0) return RA_ERR_INVALID_ARG;
+    if ((int64_t)p->max_blocks_per_seq * p->block_size > INT32_MAX) return RA_ERR_INVALID_ARG;
+    if (p->max_context_len > (int64_t)p->max_blocks_per_seq * p->block_size)
+        return RA_ERR_INVALID_ARG;
+    if (p->head_dim != 64 && p->head_dim != 128) return RA_ERR_UNSUPPORTED;
+    const int g = p->num_q_heads / p->num_kv_heads;
+    if (g < 1 || g > 8) return RA_ERR_UNSUPPORTED;
+    if ((int64_t)total_q * p->num_q_heads > (1 << 28)) return RA_ERR_UNSUPPORTED;
+    return RA_OK;
+}
+
+}  // namespace ra

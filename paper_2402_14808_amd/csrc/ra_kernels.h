@@ -67,6 +67,7 @@ struct TileArgs {                // both partial attentions of a decode step in 
     int ctx_light_begin, ctx_light_waves, sys_wg_tiles, sys_tiles_total;
     int block_size_log2, max_blocks_per_seq, rows;
     int sys_head_fastest;        // system item order: kv head varies fastest (token-major cache)
+    int fp4;                     // the context cache holds 4-bit codes
     float scale_log2;
     // Measurement aid: when not null, wavefront w of the launch (4 per workgroup) stores the
     // 100 MHz counter at its begin and its end in timeline[2w], timeline[2w+1] (w < timeline_waves).
@@ -115,6 +116,7 @@ struct RowsArgs {                // many query rows per kv head: prompt phase, w
     int n_tokens, Hq, Hkv, G, sys_len, sys_chunk, n_sys_chunks, n_sys_rowblocks, n_sys_items;
     int ctx_part, n_ctx_parts, n_ctx_rowblocks, n_ctx_items;
     int block_size_log2, max_blocks_per_seq, rows, sys_head_fastest;
+    int fp4;                     // the context cache holds 4-bit codes
     float scale_log2;
     // Several shared prefixes in the prompt phase (0 or 1: the fields above describe the only
     // one): prefix p owns the packed tokens pfx_tok0[p] .. +pfx_ntok[p]-1 (its requests are
@@ -133,6 +135,23 @@ struct AppendArgs {              // cache append (Alg. 1: write the new K,V befo
     const int32_t *block_tables, *context_lens, *cu_seqlens_q;
     int64_t new_stride_token, new_stride_head;
     int batch, total_q, Hkv, head_dim, block_size_log2, max_blocks_per_seq;
+};
+
+struct Fp4RowsArgs {             // rows into the 4-bit context cache, or out of it (fp4_cache.hip)
+    uint16_t *k_rows, *v_rows;   // bf16 [n_tokens][Hkv][head_dim]; read only when they are the new rows
+    uint8_t *k_cache, *v_cache;
+    const int32_t *slot_map;     // place of each token, or null: by the three arrays below
+    const int32_t *block_tables, *context_lens, *cu_seqlens_q;
+    int64_t stride_token, stride_head, n_slots;
+    int batch, n_tokens, Hkv, block_size_log2, max_blocks_per_seq;
+};
+
+struct TableArgs {               // block tables and slots from request lengths (tables.hip)
+    const int32_t *old_lens, *new_lens, *pool_in;
+    int32_t *pool_out, *free_blocks, *block_tables, *context_lens;
+    int32_t *cu_seqlens_q;       // may be null
+    int32_t *slot_map;           // [n_slots]
+    int batch, num_blocks, block_size_log2, max_blocks_per_seq, n_slots;
 };
 
 struct SysFillArgs {             // offline fill of the shared system cache (Sec. 3.3)
@@ -163,6 +182,8 @@ hipError_t launch_relay_tiles(const TileArgs &a, int head_dim, hipStream_t strea
 hipError_t launch_decode_direct(const DirectArgs &a, const DirectOne *one, const DirectMany *many, int head_dim,
                                 hipStream_t stream);
 hipError_t launch_cache_append(const AppendArgs &a, hipStream_t stream);
+hipError_t launch_fp4_rows(const Fp4RowsArgs &a, int head_dim, bool read, hipStream_t stream);
+hipError_t launch_update_tables(const TableArgs &a, hipStream_t stream);
 hipError_t launch_system_fill(const SysFillArgs &a, hipStream_t stream);
 
 struct ValidateArgs {            // device-side range check of lengths and block ids

@@ -8,6 +8,7 @@
 #include <cmath>
 #include <mutex>
 
+#include "ra_host.h"
 #include "ra_kernels.h"
 
 // Scratch of relay_attn_decode_static: the partial results between the partial-attention launch
@@ -16,6 +17,10 @@
 // code the name is only a handle for hipGetSymbolAddress, never an address to pass on.
 constexpr size_t kStaticScratchBytes = (size_t)32 << 20;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
+
+using ra::aligned16;
+using ra::check_params;
+using ra::kFp4LeastBlock;
 
 namespace {
 
@@ -49,33 +54,6 @@ struct Plan {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-ra_status check_params(const ra_params *p, int32_t total_q) {
-    if (!p) return RA_ERR_INVALID_ARG;
-    if (p->batch < 0 || total_q < 0 || p->num_q_heads < 1 || p->num_kv_heads < 1 ||
-        p->sys_len < 0 || p->block_size < 1 || p->num_blocks < 0 || p->max_blocks_per_seq < 0 ||
-        p->max_context_len < 0 || p->sys_chunk_tokens < 0 || p->ctx_part_tokens < 0 ||
-        p->reserved0 != 0)
-        return RA_ERR_INVALID_ARG;
-    if (p->num_q_heads % p->num_kv_heads != 0) return RA_ERR_INVALID_ARG;
-    if ((p->block_size & (p->block_size - 1)) != 0) return RA_ERR_INVALID_ARG;
-    if (!(p->softmax_scale == p->softmax_scale)) return RA_ERR_INVALID_ARG;  // NaN
-    if (p->out_is_fp32 != 0 && p->out_is_fp32 != 1) return RA_ERR_INVALID_ARG;
-    const int64_t strides[] = {p->q_stride_token, p->q_stride_head, p->o_stride_token,
-                               p->o_stride_head, p->sys_stride_token, p->sys_stride_head};
-    for (int64_t s : strides)
-        if (s < 0 || (s % 8) != 0) return RA_ERR_INVALID_ARG;
-    if (p->sys_chunk_tokens % 32 != 0 || p->ctx_part_tokens % 128 != 0) return RA_ERR_INVALID_ARG;
-    if ((int64_t)p->max_blocks_per_seq * p->block_size > INT32_MAX) return RA_ERR_INVALID_ARG;
-    if (p->max_context_len > (int64_t)p->max_blocks_per_seq * p->block_size)
-        return RA_ERR_INVALID_ARG;
-    if (p->head_dim != 64 && p->head_dim != 128) return RA_ERR_UNSUPPORTED;
-    const int g = p->num_q_heads / p->num_kv_heads;
-    if (g < 1 || g > 8) return RA_ERR_UNSUPPORTED;
-    if ((int64_t)total_q * p->num_q_heads > (1 << 28)) return RA_ERR_UNSUPPORTED;
-    return RA_OK;
-}
 
 enum PlanKind { kRelayDecode, kNaiveDecode, kPrefill };
 
@@ -696,9 +674,10 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
               bool naive, int32_t num_prefixes = 0, const ra_prefix *prefixes = nullptr,
               int phases = 3, const NewRows *append = nullptr,
               const int32_t *req_order = nullptr, const int32_t *req_prefix = nullptr,
-              const int32_t *prefix_num_tokens = nullptr, const Timeline *timeline = nullptr) {
+              const int32_t *prefix_num_tokens = nullptr, const Timeline *timeline = nullptr, bool fp4 = false) {
     ra_status st = check_params(p, total_q);
     if (st != RA_OK) return st;
+    if (fp4 && p->block_size < kFp4LeastBlock) return RA_ERR_UNSUPPORTED;
     if (naive && p->sys_len != 0) return RA_ERR_INVALID_ARG;
     if (append) {
         if (append->stride_token < 0 || append->stride_head < 0 || append->stride_token % 8 ||
@@ -788,7 +767,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
 
     // A small decode step in one launch.  (A timeline is one of the two-launch form: it is taken of the partial
     // attention, and the result is this form's all the same.)
-    const bool direct_step = !naive && !prefill && mask == 3 && direct_form(p, total_q, pl.max_ctx, groups.sys_len);
+    const bool direct_step = !naive && !prefill && !fp4 && mask == 3 && direct_form(p, total_q, pl.max_ctx, groups.sys_len);
     auto launch_direct_step = [&]() -> ra_status {
         ra::DirectArgs d{};
         d.q = static_cast<const uint16_t *>(q);
@@ -878,6 +857,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         r.rows = pl.rows;
         r.sys_head_fastest = head_fastest;
         r.scale_log2 = scale_log2;
+        r.fp4 = fp4 ? 1 : 0;
         r.n_prefixes = num_prefixes;
         r.batch = p->batch;
         r.whole = whole ? 1 : 0;
@@ -1004,6 +984,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         t.rows = pl.rows;
         t.sys_head_fastest = head_fastest;
         t.scale_log2 = scale_log2;
+        t.fp4 = fp4 ? 1 : 0;
         if (timeline) t.timeline = timeline->entries, t.timeline_waves = timeline->waves;
         if (ra::launch_relay_tiles(t, p->head_dim, stream) != hipSuccess) return RA_ERR_HIP;
         if (direct_step) return launch_direct_step();
@@ -1373,6 +1354,29 @@ ra_status relay_attn_cache_append(const ra_params *p, const void *k_new, const v
     if (ra::launch_cache_append(a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return RA_ERR_HIP;
     return RA_OK;
+}
+
+ra_status relay_attn_decode_fp4(const ra_params *p, const void *q, const void *k_sys, const void *v_sys,
+                                const void *k_cache, const void *v_cache, const int32_t *block_tables,
+                                const int32_t *context_lens, void *out, float *lse_out, void *workspace,
+                                size_t workspace_bytes, void *hip_stream) {
+    if (!p) return RA_ERR_INVALID_ARG;
+    return run(p, q, nullptr, p->batch, 1, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out, lse_out,
+               workspace, workspace_bytes, hip_stream, false, 0, nullptr, 3, nullptr, nullptr, nullptr, nullptr,
+               nullptr, true);
+}
+
+ra_status relay_attn_prefill_fp4(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, int32_t total_q,
+                                 int32_t max_q_len, const void *k_sys, const void *v_sys, const void *k_cache,
+                                 const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
+                                 void *out, float *lse_out, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream) {
+    if (!p || max_q_len < 0 || total_q < 0) return RA_ERR_INVALID_ARG;
+    if (total_q > 0 && (!cu_seqlens_q || p->batch < 1)) return RA_ERR_INVALID_ARG;
+    if ((int64_t)max_q_len * p->batch < total_q) return RA_ERR_INVALID_ARG;
+    return run(p, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out,
+               lse_out, workspace, workspace_bytes, hip_stream, false, 0, nullptr, 3, nullptr, nullptr, nullptr,
+               nullptr, nullptr, true);
 }
 
 ra_status relay_attn_system_cache_layout(const ra_params *p, int64_t *stride_token_out,

@@ -28,12 +28,12 @@
 
 namespace ra {
 
-template <int D, bool MULTI, bool WHOLE>
+template <int D, bool MULTI, bool WHOLE, bool FP4 = false>
 __global__ __launch_bounds__(kThreads, 2) void relay_rows_kernel(const RowsArgs a) {
     const unsigned long long t_begin = a.timeline ? __builtin_amdgcn_s_memrealtime() : 0ull;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * 2 * 64 * D * 2];
     __shared__ int32_t sm_tbl[kMaxPartBlocks];
-    rows_item<D, false, MULTI, WHOLE>(a, (int)blockIdx.x, lds, sm_tbl);
+    rows_item<D, false, MULTI, WHOLE, FP4>(a, (int)blockIdx.x, lds, sm_tbl);
     if (a.timeline) {
         const unsigned w = blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
         if (threadIdx.x % kWave == 0 && w < (unsigned)a.timeline_waves) {
@@ -49,12 +49,17 @@ hipError_t launch_relay_rows(const RowsArgs &a, int head_dim, hipStream_t stream
     if (groups > INT32_MAX) return hipErrorInvalidValue;
     const bool multi = a.n_prefixes > 1;
     if (a.whole && (a.n_sys_chunks != 1 || !a.cu_seqlens_q || !a.out)) return hipErrorInvalidValue;
+    if (a.fp4 && multi) return hipErrorInvalidValue;           // (no entry point asks for it)
     const dim3 grid((unsigned)groups), block(kThreads);
 #define RA_ROWS(D_, MULTI_, WHOLE_) \
     hipLaunchKernelGGL((relay_rows_kernel<D_, MULTI_, WHOLE_>), grid, block, 0, stream, a)
+#define RA_ROWS_FP4(D_, WHOLE_) \
+    hipLaunchKernelGGL((relay_rows_kernel<D_, false, WHOLE_, true>), grid, block, 0, stream, a)
 #define RA_ROWS_D(D_)                               \
     do {                                            \
-        if (a.whole && multi) RA_ROWS(D_, true, true);   \
+        if (a.fp4 && a.whole) RA_ROWS_FP4(D_, true);     \
+        else if (a.fp4) RA_ROWS_FP4(D_, false);     \
+        else if (a.whole && multi) RA_ROWS(D_, true, true);   \
         else if (a.whole) RA_ROWS(D_, false, true); \
         else if (multi) RA_ROWS(D_, true, false);   \
         else RA_ROWS(D_, false, false);             \
@@ -63,6 +68,7 @@ hipError_t launch_relay_rows(const RowsArgs &a, int head_dim, hipStream_t stream
     else if (head_dim == 64) RA_ROWS_D(64);
     else return hipErrorInvalidValue;
 #undef RA_ROWS_D
+#undef RA_ROWS_FP4
 #undef RA_ROWS
     return hipGetLastError();
 }

@@ -35,6 +35,7 @@
 // so any block placement of the same cache gives bit-identical results.  Rows past the end of
 // an item are never loaded (their lanes re-load the item's last row and the scores are masked);
 // block-table slots past the last used block may be read but are never dereferenced.
+#include "fp4_attend.h"
 #include "ra_device.h"
 #include "ra_kernels.h"
 #include "rows_item.h"
@@ -488,7 +489,7 @@ __device__ __forceinline__ int wave_inclusive_scan(int x, int lane) {
 // light wavefronts take nothing where the others can take all tiles at the floor, and all spans are
 // equal otherwise.  60 requests of 32/8 heads, s = 4096, contexts of 500 .. 2000 under a bound of 17392,
 // 64 system workgroups of 128 tiles: 87.8 us with work next to them, 72.4 without.
-template <int D, bool APPEND>
+template <int D, bool APPEND, bool FP4>
 __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned char *smem,
                                                  float (*sm_m)[32], float (*sm_l)[32],
                                                  int32_t (*sm_tbl)[kMaxPartBlocks]) {
@@ -676,6 +677,10 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
             asm volatile("" : "+v"(next));
             a.part_lse[(int64_t)next * a.rows + row] = __uint_as_float(kEndOfPartials);
         }
+        if constexpr (FP4) {
+            fp4_attend<D>(a, req, g, 32 * (int)j, min(c_req, 32 * (int)(j + seg)), a.n_sys_chunks + slot, lane_here,
+                          sm_tbl[wave]);
+        } else {
         Item it;
         it.g = g;
         it.key_begin = 32 * (int)j;
@@ -685,6 +690,7 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
         it.append_pos = APPEND && j + seg == T ? c_req - 1 : -1;   // (-1 for an empty context)
         it.mt = 0; it.tok0 = 0; it.ncols = a.G; it.k = nullptr; it.v = nullptr;
         attend<D, false, true, APPEND>(a, it, lane_here, smem, sm_m, sm_l, sm_tbl);   // rows are read once
+        }
         x += seg;
         if (x >= x1) break;
         j = 0;
@@ -707,7 +713,8 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
 // B*G stacked rows per kv head are many row tiles that would each pull the whole system K/V into
 // their compute unit: what a unit can draw, from HBM or from L2, is the bound of this launch.
 // APPEND: the context wavefronts also perform the cache write of the decode step (k_new / v_new).
-template <int D, bool SYS_NT, bool MULTI, bool ROWS, bool APPEND>
+// FP4: the context cache holds 4-bit codes (fp4_attend.h); the system prompt is bfloat16 as ever.
+template <int D, bool SYS_NT, bool MULTI, bool ROWS, bool APPEND, bool FP4 = false>
 __global__ __launch_bounds__(kThreads, 2) void relay_tile_kernel(const TileArgs a) {
     const unsigned long long t_begin = a.timeline ? __builtin_amdgcn_s_memrealtime() : 0ull;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * TileCfg<D>::SLICE];
@@ -750,7 +757,7 @@ __global__ __launch_bounds__(kThreads, 2) void relay_tile_kernel(const TileArgs 
         // through (grouped-query shape with many-rows system items 75 -> 71 us, Llama-30B shape at
         // a 2048-position prompt 34.2 -> 33.4 us).
         __builtin_amdgcn_s_setprio(3);
-        run_context_wave<D, APPEND>(a, smem, sm_m, sm_l, sm_tbl);
+        run_context_wave<D, APPEND, FP4>(a, smem, sm_m, sm_l, sm_tbl);
     }
     if (a.timeline) {
         const unsigned w = blockIdx.x * kWaves + threadIdx.x / kWave;
@@ -773,11 +780,19 @@ hipError_t launch_relay_tiles(const TileArgs &a, int head_dim, hipStream_t strea
     if (append && multi) return hipErrorInvalidValue;          // (no entry point asks for it)
     const bool rows = a.n_sys_rowblocks > 0;                   // system items of the many-rows kind
     if (rows && multi) return hipErrorInvalidValue;
+    const bool fp4 = a.fp4 != 0;
+    if (fp4 && (append || multi)) return hipErrorInvalidValue;
 #define RA_LAUNCH(D_, NT_, MULTI_, ROWS_, APPEND_) \
     hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, MULTI_, ROWS_, APPEND_>), grid, block, 0, stream, a)
+#define RA_LAUNCH_FP4(D_, NT_, ROWS_) \
+    hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, false, ROWS_, false, true>), grid, block, 0, stream, a)
 #define RA_PICK(D_)                                                         \
     do {                                                                    \
-        if (rows) {                                                         \
+        if (fp4) {                                                          \
+            if (rows) RA_LAUNCH_FP4(D_, false, true);                       \
+            else if (sys_nt) RA_LAUNCH_FP4(D_, true, false);                \
+            else RA_LAUNCH_FP4(D_, false, false);                           \
+        } else if (rows) {                                                         \
             if (append) RA_LAUNCH(D_, false, false, true, true);            \
             else RA_LAUNCH(D_, false, false, true, false);                  \
         } else if (append) {                                                \
@@ -795,6 +810,7 @@ hipError_t launch_relay_tiles(const TileArgs &a, int head_dim, hipStream_t strea
     else if (head_dim == 64) RA_PICK(64);
     else return hipErrorInvalidValue;
 #undef RA_PICK
+#undef RA_LAUNCH_FP4
 #undef RA_LAUNCH
     return hipGetLastError();
 }

@@ -2,6 +2,7 @@
 // (relay_rows.hip) and the decode launch for wide grouped-query batches (relay_tiles.hip, where
 // system items of this kind share the launch with the context wavefronts) run the same code.
 #pragma once
+#include "fp4.h"
 #include "ra_device.h"
 #include "ra_kernels.h"
 
@@ -45,7 +46,10 @@ constexpr float kLazyLog2 = 8.0f;
 // neither partials nor a fusion launch are needed (Alg. 1's relay fusion becomes the running
 // rescale of one online softmax over [system ; context], which is the same number).  The host
 // picks it when the system prompt is one chunk and the requests bring many new tokens each.
-template <int D, bool SYS_ONLY, bool MULTI = false, bool WHOLE = false>
+// FP4: the context cache holds 4-bit codes.  The system prompt's steps are loaded as ever; a context step's codes land in
+// registers while the step before is worked off and go to the other buffer as bfloat16 (exactly, see fp4.h) when it
+// is done, in the same places.
+template <int D, bool SYS_ONLY, bool MULTI = false, bool WHOLE = false, bool FP4 = false>
 __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, unsigned char *lds,
                                           int32_t *sm_tbl) {
     constexpr int ROW_BYTES = D * 2;
@@ -195,7 +199,49 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
     // its rows to the item's end; context items find their rows through the block table.
     int64_t run_off = (int64_t)(key_begin + lrow) * a.sys_stride_token;
     const int64_t rpl_stride = (int64_t)RPL * a.sys_stride_token;
+    // FP4: of a step's 64 rows of K and of V a thread takes pieces of one block of 32 values (16 bytes of codes and a scale):
+    // one of K and one of V (d = 128), or one of K or of V (64).  Piece c of row r is 64-byte segment c there.
+    constexpr int PIECES = D / 64;
+    constexpr int PPR = D / 32;                   // pieces of a row
+    [[maybe_unused]] u32x4 codes[PIECES];
+    [[maybe_unused]] uint32_t scales[PIECES];
+    [[maybe_unused]] const int piece = D == 128 ? threadIdx.x : threadIdx.x & 127;
+    [[maybe_unused]] const bool piece_is_v = D == 64 && threadIdx.x >= 128;      // (d = 128: K first, then V)
+    [[maybe_unused]] const int prow = piece / PPR, pcol = piece % PPR;
+    auto load_codes = [&](int tile0) {
+        const int key = min(tile0 + prow, key_end - 1);
+        const int64_t blk = sm_tbl[(key >> bsl) - first_blk];
+        const int64_t at = (blk * a.Hkv + g) * Fp4<D>::block_bytes(bsl);
+        const int off = key & bmask;
+        const int64_t code_at = at + off * Fp4<D>::ROW + pcol * 16;
+        const int64_t scale_at = at + ((int64_t)Fp4<D>::ROW << bsl) + (pcol << bsl) + off;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint8_t *cache = reinterpret_cast<const uint8_t *>((D == 64 ? piece_is_v : i == 1) ? a.v_cache : a.k_cache);
+            codes[i] = *reinterpret_cast<const u32x4 *>(cache + code_at);
+            scales[i] = cache[scale_at];
+        }
+    };
+    auto store_codes = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const bool is_v = D == 64 ? piece_is_v : i == 1;
+            const float e = fp4_scale(scales[i]);
+            RA_ROWS_LDS unsigned char *row = lds3 + buf * (2 * KV_BYTES) + (is_v ? KV_BYTES : 0) + prow * ROW_BYTES;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int pos = is_v ? ((pcol ^ (prow & (SEGS - 1))) << 2) | w : (4 * pcol + w) ^ (prow & (CPR - 1));
+                *(RA_ROWS_LDS u32x4 *)(row + pos * 16) = fp4_octet(codes[i][w], e);
+            }
+        }
+    };
     auto load_step = [&](int tile0, int buf) {
+        if constexpr (FP4) {
+            if (!is_sys) {
+                load_codes(tile0);
+                return;
+            }
+        }
         const uint32_t kb = lds_wave + (uint32_t)buf * (2 * KV_BYTES);
         if (is_sys && tile0 + STEP <= key_end) {
 #pragma unroll
@@ -280,6 +326,9 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
     auto run_range = [&]() {
     if (key_begin < key_end) {
         load_step(key_begin, 0);
+        if constexpr (FP4) {
+            if (!is_sys) store_codes(0);
+        }
         loads_landed();
     }
     __syncthreads();
@@ -411,6 +460,9 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
             weights(sb, pb_, pb_lo);
             accumulate(0, pa, pa_lo);
             accumulate(32, pb_, pb_lo);
+        }
+        if constexpr (FP4) {
+            if (!is_sys && tile0 + STEP < key_end) store_codes(buf ^ 1);
         }
         loads_landed();
         __syncthreads();   // next step visible to all; everyone is done reading this one
