@@ -2,15 +2,17 @@
 // wavefront per span (Eq. 7, second term; the format: fp4.h).
 //
 // A tile is 32 positions.  Both products run on v_mfma_f32_16x16x32_bf16 with the values converted on the way from the
-// registers the loads landed in: nothing passes through LDS.  What makes that possible is that the contraction index of a
+// registers the loads landed in.  What makes that possible is that the contraction index of a
 // matrix product may be numbered at will as long as both operands agree:
 //   S^T = K Q^T   Row m of product u (0, 1) is position 8 (m / 4) + 4 u + m % 4 of the tile.  Lane (m, h) holds a quarter
 //                 of that position's channels, D/4 from h D/4 on: 16 (d = 64: 8) bytes of codes, one load, one scale
 //                 (32 channels or half of them).  Word n of it is the operand of step n as it stands.
 //   O^T += V^T P^T  S^T leaves lane (col, h) with positions 8 h .. 8 h + 7 of query head `col`, which is what the operand
-//                 P^T wants of it.  So V^T's operand is 8 positions of a channel per lane: lane (i, h) loads the
+//                 P^T wants of it.  So V^T's operand is 8 positions of a channel per lane: lane (i, h) takes the
 //                 word of channels 8 i .. 8 i + 7 of its 8 positions, converts two codes at a time and swaps
-//                 halves between two positions (v_perm_b32); product n gets channel 8 i + n.
+//                 halves between two positions (v_perm_b32); product n gets channel 8 i + n.  The words come through the
+//                 wavefront's own LDS: loaded as they are needed, 4 bytes a lane, they held the loads of a launch to 5.4
+//                 TB/s (d = 128) and 4.0 (64), 16 bytes a lane to 6.2 and more.
 // The rows' powers of two are part of the conversions, so both operands are exact, and P is split into a high
 // and a low bfloat16 part as in the bf16 kernels.
 // Bound: HBM.  A tile is 4.25 KiB (d = 128) and some 200 vector instructions.
@@ -37,19 +39,29 @@ __device__ __forceinline__ float sum_with_other_row(float x) {
 constexpr float kFp4LazyLog2 = 8.0f;              // see kLazyLog2 in rows_item.h
 
 // Positions [key_begin, key_end) (key_begin a multiple of 32) of request `req`, kv head g, into partial `part_index`.
-// `tbl`: kMaxPartBlocks entries of LDS that belong to the wavefront.
+// `lds`: Fp4Lds<D>::BYTES bytes that belong to the wavefront, aligned to 16.
+constexpr int kFp4TableEntries = kMaxPartBlocks + 32 / 8;
+template <int D>
+struct Fp4Lds {                                   // of the two tiles in turn
+    static constexpr int TABLE = kFp4TableEntries * 8;
+    static constexpr int V_TILE = 36 * Fp4<D>::ROW;             // rows, each eight of them one row further: no bank conflicts
+    static constexpr int S_TILE = 2 * Fp4<D>::GROUPS * 32;      // scales [K, V][group][position]
+    static constexpr int V_AT = TABLE, S_AT = V_AT + 2 * V_TILE, BYTES = S_AT + 2 * S_TILE;
+};
 template <int D>
 __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, const int g, const int key_begin,
-                                           int key_end, const int part_index, const int lane, int32_t *tbl) {
+                                           int key_end, const int part_index, const int lane, unsigned char *lds) {
     constexpr int KW = D / 32;                    // code words of a lane's part of a K row; steps of S^T
     constexpr int NT = D / 16;                    // products of O^T
     constexpr int ROW = Fp4<D>::ROW;
     const int col = lane & 15, h = lane >> 4;
     const int bsl = a.block_size_log2, bmask = (1 << bsl) - 1;
-    const int64_t block_bytes = Fp4<D>::block_bytes(bsl);
     const int scales_at = ROW << bsl;
+    using L = Fp4Lds<D>;
+    int64_t *tbl = reinterpret_cast<int64_t *>(lds);
 
-    // block ids of the span
+    // Where the blocks of the span begin, in bytes.  Behind the last one it is named again, so that a tile that ends in
+    // it finds an address for its missing rows.
     const int first_blk = key_begin >> bsl;
     {
         int nblk = key_end > key_begin ? ((key_end - 1) >> bsl) - first_blk + 1 : 0;
@@ -57,7 +69,9 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         nblk = min(nblk, min(kMaxPartBlocks, a.max_blocks_per_seq - first_blk));
         key_end = min(key_end, (first_blk + nblk) << bsl);
         const int32_t *bt = a.block_tables + (int64_t)req * a.max_blocks_per_seq + first_blk;
-        for (int j = lane; j < nblk; j += kWave) tbl[j] = bt[j];
+        if (nblk > 0)
+            for (int j = lane; j < nblk + 32 / 8; j += kWave)
+                tbl[j] = ((int64_t)bt[min(j, nblk - 1)] * a.Hkv + g) * Fp4<D>::block_bytes(bsl);
     }
 
     // Q^T: channels h D/4 + 8 n .. + 7 of head `col`.  A negative scale goes into its sign; a zero one becomes
@@ -76,44 +90,64 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         qf[n] = __builtin_bit_cast(bf16x8, w);
     }
 
-    const uint8_t *k_cache = reinterpret_cast<const uint8_t *>(a.k_cache);
-    const uint8_t *v_cache = reinterpret_cast<const uint8_t *>(a.v_cache);
-    const int oct = D == 128 ? col : col & 7;     // V: the word of a row that this lane takes
-    const int k_group = h * (D / 4) / 32, v_group = oct / 4;
+    // A lane loads quarter h of positions kp and kp + 4 of K and of V (eight positions that begin at a multiple of eight lie
+    // in one block), and four scales: of K in the lower lanes and of V in the upper ones (d = 64 has half as many, and takes
+    // them twice).  Rows behind the end are loaded like the others, whatever they hold: scores and powers of two
+    // are put right below.
+    const int oct = D == 128 ? col : col & 7;     // V: the word of a row that this lane multiplies
+    const int kp = 8 * (col >> 2) + (col & 3);
+    const int sl = D == 128 ? lane : lane & 31;   // scales: cache, group, positions 4 (sl % 8) ..
+    const int s_group = (sl >> 3) & (Fp4<D>::GROUPS - 1), s_pos = 4 * (sl & 7);
+    const bool s_is_v = sl >= 8 * Fp4<D>::GROUPS;
+    const int64_t lane_at = (kp & bmask) * ROW + h * (KW * 4);
+    const uint8_t *k_codes = reinterpret_cast<const uint8_t *>(a.k_cache) + lane_at;
+    const uint8_t *v_codes = reinterpret_cast<const uint8_t *>(a.v_cache) + lane_at;
+    const uint8_t *scale_bytes = reinterpret_cast<const uint8_t *>(s_is_v ? a.v_cache : a.k_cache) + scales_at +
+                                 (s_group << bsl) + (s_pos & bmask);
+    const int64_t *code_tbl = tbl + (kp >> bsl), *scale_tbl = tbl + (s_pos >> bsl);
+    uint32_t *const s_put = reinterpret_cast<uint32_t *>(lds + L::S_AT + 4 * sl);
+    unsigned char *const v_put = lds + L::V_AT + kp * ROW + (kp >> 3) * ROW + h * (KW * 4);
+    const unsigned char *const v_get = lds + L::V_AT + 9 * h * ROW + oct * 4;
+    const unsigned char *const ks_get = lds + L::S_AT + (h * (D / 4) / 32) * 32 + (kp & ~7);
+    const unsigned char *const vs_get = lds + L::S_AT + (Fp4<D>::GROUPS + oct / 4) * 32 + 8 * h;
 
     struct Tile {
-        uint32_t k[2][KW], k_scale[2], v[8];
-        u32x2 v_scale;                            // of positions 8 h .. 8 h + 7, a byte each
+        uint32_t k[2][KW], v[2][KW], scales;
     };
-    auto block_of = [&](int key) { return ((int64_t)tbl[(key >> bsl) - first_blk] * a.Hkv + g) * block_bytes; };
+    const int last_tile = key_begin + ((key_end - key_begin - 1) & ~31);
+    auto load_words = [](const uint8_t *from, uint32_t (&w)[KW]) {       // (rows are read once: non-temporal)
+        if constexpr (KW == 4) {
+            const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from));
+#pragma unroll
+            for (int n = 0; n < KW; ++n) w[n] = x[n];
+        } else {
+            const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(from));
+#pragma unroll
+            for (int n = 0; n < KW; ++n) w[n] = x[n];
+        }
+    };
     auto load = [&](int tile0, Tile &t) {
-        // Rows behind the end re-load the last one; V words come eight positions at a time, which lie in one block
-        // (block_size >= 8), so that the ones behind the end there are read, and count for nothing.
-        const int last = key_end - 1;
+        tile0 = min(tile0, last_tile);            // (as many loads each time: the waits count them)
+        const int blk = (tile0 >> bsl) - first_blk, off = tile0 & bmask;
+        const int64_t at = code_tbl[blk] + off * ROW, scales_of = scale_tbl[blk] + off;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int key = min(tile0 + 8 * (col >> 2) + 4 * u + (col & 3), last);
-            const uint8_t *block = k_cache + block_of(key);
-            const int off = key & bmask;
-            const uint8_t *src = block + off * ROW + h * (KW * 4);
-            if constexpr (KW == 4) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(src);
-#pragma unroll
-                for (int n = 0; n < KW; ++n) t.k[u][n] = w[n];
-            } else {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(src);
-#pragma unroll
-                for (int n = 0; n < KW; ++n) t.k[u][n] = w[n];
-            }
-            t.k_scale[u] = block[scales_at + (k_group << bsl) + off];
+            load_words(k_codes + at + 4 * u * ROW, t.k[u]);
+            load_words(v_codes + at + 4 * u * ROW, t.v[u]);
         }
-        const int key = min(tile0 + 8 * h, last & ~7);
-        const uint8_t *block = v_cache + block_of(key);
-        const int off = key & bmask;
-        const uint8_t *src = block + off * ROW + oct * 4;
+        t.scales = *reinterpret_cast<const uint32_t *>(scale_bytes + scales_of);
+    };
+    auto through_lds = [&](const Tile (&t)[2]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t.v[j] = *reinterpret_cast<const uint32_t *>(src + j * ROW);
-        t.v_scale = *reinterpret_cast<const u32x2 *>(block + scales_at + (v_group << bsl) + off);
+        for (int x = 0; x < 2; ++x) {
+            s_put[x * (L::S_TILE / 4)] = t[x].scales;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                unsigned char *to = v_put + x * L::V_TILE + 4 * u * ROW;
+                if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(to) = u32x4{t[x].v[u][0], t[x].v[u][1], t[x].v[u][2], t[x].v[u][3]};
+                else *reinterpret_cast<u32x2 *>(to) = u32x2{t[x].v[u][0], t[x].v[u][1]};
+            }
+        }
     };
 
     f32x4 acc[NT];
@@ -121,33 +155,45 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
     for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, msc = 0.f, l_run = 0.f;
 
-    auto compute = [&](int tile0, const Tile &t) {
-        f32x4 s[2];
+    auto compute = [&](int tile0, const Tile (&t)[2]) {       // two tiles: their chains of products are independent
+        through_lds(t);
+        u32x2 v_scale[2];
+        f32x4 s[4];                               // s[2 x + u]: product u of tile x
+        float ks[4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const float ks = fp4_scale(t.k_scale[u]);
-#pragma unroll
-            for (int n = 0; n < KW; ++n)
-                s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp4_octet(t.k[u][n], ks)), qf[n],
-                                                               s[u], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+            s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // byte kp % 4 of the word to bits 23 .. 30 (the conversions read no other)
+            const uint32_t word = *reinterpret_cast<const uint32_t *>(ks_get + (i / 2) * L::S_TILE + 4 * (i & 1));
+            ks[i] = __uint_as_float(__builtin_amdgcn_alignbit(word, word, (8 * (col & 3) + 9) & 31));
         }
-        u32x2 v_scale = t.v_scale;
-        if (tile0 + 32 > key_end) {               // ragged last tile: no weight and a harmless power of two behind the end
-            const int mine = min(max(key_end - (tile0 + 8 * h), 0), 8);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+        for (int n = 0; n < KW; ++n)              // (the four chains in turn: a product that waits for the one before it stalls)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[u][r] = 4 * u + r < mine ? s[u][r] : -INFINITY;
+            for (int i = 0; i < 4; ++i)
+                s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8, fp4_octet(t[i / 2].k[i & 1][n], ks[i])), qf[n], s[i], 0, 0, 0);
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int bytes = min(max(mine - 4 * w, 0), 4);
-                const uint32_t word = v_scale[w];
-                v_scale[w] = bytes == 4 ? word : word & ((1u << (8 * bytes)) - 1u);
+        for (int x = 0; x < 2; ++x) v_scale[x] = *reinterpret_cast<const u32x2 *>(vs_get + x * L::S_TILE);
+        if (tile0 + 64 > key_end) {               // ragged end: no weight and a harmless power of two behind it
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int mine = min(max(key_end - (tile0 + 32 * x + 8 * h), 0), 8);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[2 * x + u][r] = 4 * u + r < mine ? s[2 * x + u][r] : -INFINITY;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const int bytes = min(max(mine - 4 * w, 0), 4);
+                    const uint32_t word = v_scale[x][w];
+                    v_scale[x][w] = bytes == 4 ? word : word & ((1u << (8 * bytes)) - 1u);
+                }
             }
         }
-        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                         fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])));
         // The maximum that the sums are expressed against moves when a column outgrew it by the margin or sees its
         // first key; only then do the four lanes of a column have to agree on it.
         if (__builtin_amdgcn_ballot_w64(mx > m_run + lazy_raw) != 0) {
@@ -161,59 +207,68 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
             m_run = m_new;
             msc = msc_new;
         }
-        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i / 2][2 * (i & 1)], scale, -msc));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[i / 2][2 * (i & 1) + 1], scale, -msc));
-            l_run += p0 + p1;
-            hi[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
-            lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - bf16_lo(hi[i]), p1 - bf16_hi(hi[i])}), bf16x2));
-        }
-        const bf16x8 ph = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
-        const bf16x8 pl = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
-
-        float vs[8];
+        for (int x = 0; x < 2; ++x) {
+            uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) vs[j] = fp4_scale((v_scale[j / 4] >> (8 * (j & 3))) & 0xffu);
-        uint32_t w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = D == 128 ? t.v[j] : t.v[j] >> (16 * (col >> 3));
-        auto products = [&](auto byte_tag) {      // channels 2 BYTE and 2 BYTE + 1 of each lane's word
-            constexpr int BYTE = decltype(byte_tag)::value;
-            u32x4 even, odd;
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const uint32_t x = fp4_pair<BYTE>(w[2 * p], vs[2 * p]), y = fp4_pair<BYTE>(w[2 * p + 1], vs[2 * p + 1]);
-                even[p] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                odd[p] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            for (int i = 0; i < 4; ++i) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * x + i / 2][2 * (i & 1)], scale, -msc));
+                const float p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * x + i / 2][2 * (i & 1) + 1], scale, -msc));
+                l_run += p0 + p1;
+                hi[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+                lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - bf16_lo(hi[i]), p1 - bf16_hi(hi[i])}), bf16x2));
             }
-            const bf16x8 ve = __builtin_bit_cast(bf16x8, even), vo = __builtin_bit_cast(bf16x8, odd);
-            acc[2 * BYTE] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph, acc[2 * BYTE], 0, 0, 0);
-            acc[2 * BYTE + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, ph, acc[2 * BYTE + 1], 0, 0, 0);
-            acc[2 * BYTE] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl, acc[2 * BYTE], 0, 0, 0);
-            acc[2 * BYTE + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, pl, acc[2 * BYTE + 1], 0, 0, 0);
-        };
-        products(std::integral_constant<int, 0>{});
-        products(std::integral_constant<int, 1>{});
-        if constexpr (D == 128) {
-            products(std::integral_constant<int, 2>{});
-            products(std::integral_constant<int, 3>{});
+            const bf16x8 ph = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
+            const bf16x8 pl = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
+            float vs[8];
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t word = v_scale[x][j / 4];
+                vs[j] = __uint_as_float((j & 3) == 3 ? word >> 1 : word << (23 - 8 * (j & 3)));
+                const uint32_t v = *reinterpret_cast<const uint32_t *>(v_get + x * L::V_TILE + j * ROW);
+                w[j] = D == 128 ? v : v >> (16 * (col >> 3));
+            }
+            auto products = [&](auto byte_tag) {  // channels 2 BYTE and 2 BYTE + 1 of each lane's word
+                constexpr int BYTE = decltype(byte_tag)::value;
+                u32x4 even, odd;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const uint32_t y0 = fp4_pair<BYTE>(w[2 * p], vs[2 * p]), y1 = fp4_pair<BYTE>(w[2 * p + 1], vs[2 * p + 1]);
+                    even[p] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
+                    odd[p] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
+                }
+                const bf16x8 ve = __builtin_bit_cast(bf16x8, even), vo = __builtin_bit_cast(bf16x8, odd);
+                acc[2 * BYTE] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph, acc[2 * BYTE], 0, 0, 0);
+                acc[2 * BYTE + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, ph, acc[2 * BYTE + 1], 0, 0, 0);
+                acc[2 * BYTE] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl, acc[2 * BYTE], 0, 0, 0);
+                acc[2 * BYTE + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, pl, acc[2 * BYTE + 1], 0, 0, 0);
+            };
+            products(std::integral_constant<int, 0>{});
+            products(std::integral_constant<int, 1>{});
+            if constexpr (D == 128) {
+                products(std::integral_constant<int, 2>{});
+                products(std::integral_constant<int, 3>{});
+            }
         }
     };
 
-    // three tiles on their way while one is worked off
-    Tile ring[4];
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-        if (key_begin + 32 * i < key_end) load(key_begin + 32 * i, ring[i]);
-    for (int tile0 = key_begin; tile0 < key_end;) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (tile0 + 96 < key_end) load(tile0 + 96, ring[(i + 3) & 3]);
-            compute(tile0, ring[i]);
-            tile0 += 32;
-            if (tile0 >= key_end) break;
+    // Two tiles on their way while two are worked off.  (Loads are made and counted on every path, so that the waits of
+    // the loop are for the tiles in turn and not for all that is on its way; a loop that is left in its middle counts as
+    // paths that come back without them.)
+    Tile even[2], odd[2];
+    auto load2 = [&](int tile0, Tile (&t)[2]) {
+        load(tile0, t[0]);
+        load(tile0 + 32, t[1]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (key_begin < key_end) {
+        load2(key_begin, even);
+        for (int tile0 = key_begin; tile0 < key_end; tile0 += 128) {
+            load2(tile0 + 64, odd);
+            compute(tile0, even);
+            load2(tile0 + 128, even);
+            if (tile0 + 64 < key_end) compute(tile0 + 64, odd);
         }
     }
 

@@ -678,8 +678,9 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
             a.part_lse[(int64_t)next * a.rows + row] = __uint_as_float(kEndOfPartials);
         }
         if constexpr (FP4) {
+            static_assert(TileCfg<D>::SLICE >= Fp4Lds<D>::BYTES, "a span works in the wavefront's slice of LDS");
             fp4_attend<D>(a, req, g, 32 * (int)j, min(c_req, 32 * (int)(j + seg)), a.n_sys_chunks + slot, lane_here,
-                          sm_tbl[wave]);
+                          smem + wave * TileCfg<D>::SLICE);
         } else {
         Item it;
         it.g = g;
