@@ -169,8 +169,9 @@ def _stream():
     import torch
     if not torch.cuda.is_initialized():
         torch.cuda.init()
+    C = torch._C
     try:                                        # the same number without a stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return C._cuda_getCurrentRawStream(C._cuda_getDevice())
     except AttributeError:                      # (names a torch release may change)
         return torch.cuda.current_stream().cuda_stream
 
@@ -427,11 +428,14 @@ def fp4_cache_shape(num_blocks, num_kv_heads, block_size, head_dim):
     return int(num_blocks), int(num_kv_heads), block.value
 
 
+# (Addresses are taken in place and strides once: a small call costs the host more than the GPU.)
 def _fp4_rows(fn, where, params, k, v, cu_seqlens_q, total_q, k_cache, v_cache, block_tables, context_lens, slot_map):
-    assert k.stride() == v.stride() and k.stride(2) == 1
-    _check(fn(ctypes.byref(params), _ptr(k), _ptr(v), int(k.stride(0)), int(k.stride(1)), _ptr(cu_seqlens_q),
-              int(total_q), _ptr(slot_map), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(context_lens),
-              _stream()), where)
+    strides = k.stride()
+    assert v.stride() == strides and strides[2] == 1
+    st = fn(ctypes.byref(params), k.data_ptr(), v.data_ptr(), strides[0], strides[1], _ptr(cu_seqlens_q), total_q,
+            _ptr(slot_map), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(block_tables), _ptr(context_lens), _stream())
+    if st != RA_OK:
+        raise RelayAttnError(st, where)
 
 
 def relay_attn_cache_append_fp4(params, k_new, v_new, cu_seqlens_q, total_q, k_cache, v_cache, block_tables,
@@ -452,19 +456,18 @@ def relay_attn_cache_read_fp4(params, k_out, v_out, cu_seqlens_q, total_q, k_cac
 
 def relay_attn_decode_fp4(params, q, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out, lse_out, workspace):
     st = load().relay_attn_decode_fp4(
-        ctypes.byref(params), _ptr(q), _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache),
-        _ptr(block_tables), _ptr(context_lens), _ptr(out), _ptr(lse_out), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream())
+        ctypes.byref(params), q.data_ptr(), _ptr(k_sys), _ptr(v_sys), k_cache.data_ptr(), v_cache.data_ptr(),
+        block_tables.data_ptr(), context_lens.data_ptr(), out.data_ptr(), _ptr(lse_out), workspace.data_ptr(),
+        workspace.nbytes, _stream())
     _check(st, "relay_attn_decode_fp4")
 
 
 def relay_attn_prefill_fp4(params, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables,
                            context_lens, out, lse_out, workspace):
     st = load().relay_attn_prefill_fp4(
-        ctypes.byref(params), _ptr(q), _ptr(cu_seqlens_q), int(total_q), int(max_q_len),
-        _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
-        _ptr(context_lens), _ptr(out), _ptr(lse_out), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream())
+        ctypes.byref(params), q.data_ptr(), _ptr(cu_seqlens_q), int(total_q), int(max_q_len),
+        _ptr(k_sys), _ptr(v_sys), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(),
+        context_lens.data_ptr(), out.data_ptr(), _ptr(lse_out), workspace.data_ptr(), workspace.nbytes, _stream())
     _check(st, "relay_attn_prefill_fp4")
 
 
@@ -480,7 +483,7 @@ def relay_attn_update_tables(params, old_lens, new_lens, pool_in, pool_out, free
                              cu_seqlens_q, slot_map):
     """int32 device tensors; cu_seqlens_q and slot_map may be None."""
     st = load().relay_attn_update_tables(
-        ctypes.byref(params), _ptr(old_lens), _ptr(new_lens), _ptr(pool_in), _ptr(pool_out), _ptr(free_blocks),
-        _ptr(block_tables), _ptr(context_lens), _ptr(cu_seqlens_q), _ptr(slot_map),
+        ctypes.byref(params), old_lens.data_ptr(), new_lens.data_ptr(), pool_in.data_ptr(), pool_out.data_ptr(),
+        free_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(cu_seqlens_q), _ptr(slot_map),
         0 if slot_map is None else slot_map.numel(), _stream())
     _check(st, "relay_attn_update_tables")

@@ -16,6 +16,7 @@
 // is why the form is for small calls only (see direct_form in relay_attn.hip for the line).
 // Vector arithmetic: with one query row there is no matrix product, and the row's 16 (head_dim 128) or 8
 // lanes sum a score by data-parallel moves.
+#include "fp4.h"
 #include "ra_device.h"
 #include "ra_kernels.h"
 
@@ -30,7 +31,9 @@ __host__ __device__ constexpr int used_slot(int row, int s, int block_size_log2)
     return row < s ? 0 : (row - s) >> block_size_log2;
 }
 
-template <int D, bool MULTI, bool APPEND>
+// FP4: the context cache holds 4-bit codes.  A lane's part of a context row is a word of codes and a scale then, which
+// become the same 8 bfloat16 when the row is worked off.
+template <int D, bool MULTI, bool APPEND, bool FP4 = false>
 __global__ __launch_bounds__(kDirectThreads, 4) void decode_direct_kernel(
     const DirectArgs a, const typename DirectPrefixes<MULTI>::type pfx) {
     constexpr int LPT = D / 8;                    // lanes per row, 8 elements (16 bytes) each
@@ -93,6 +96,17 @@ __global__ __launch_bounds__(kDirectThreads, 4) void decode_direct_kernel(
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int pos = row[u] - s;
+            if (FP4 && pos >= 0) {
+                const int64_t at = ((int64_t)blk[u] * a.Hkv + g) * Fp4<D>::block_bytes(bsl);
+                const int64_t code_at = at + (pos & bmask) * Fp4<D>::ROW + sub * 4;
+                const int64_t scale_at = at + ((int64_t)Fp4<D>::ROW << bsl) + ((sub / 4) << bsl) + (pos & bmask);
+                const uint8_t *kb = reinterpret_cast<const uint8_t *>(a.k_cache), *vb = reinterpret_cast<const uint8_t *>(a.v_cache);
+                k[u][0] = *reinterpret_cast<const uint32_t *>(kb + code_at);
+                v[u][0] = *reinterpret_cast<const uint32_t *>(vb + code_at);
+                k[u][1] = kb[scale_at];
+                v[u][1] = vb[scale_at];
+                continue;
+            }
             const bool sys = pos < 0, fresh = APPEND && pos >= 0 && pos == c - 1;   // fresh: not in the cache yet
             int64_t off = sys ? (int64_t)row[u] * a.sys_stride_token
                               : ((((int64_t)blk[u] * a.Hkv + g) << bsl) + (pos & bmask)) * (int64_t)D;
@@ -106,7 +120,15 @@ __global__ __launch_bounds__(kDirectThreads, 4) void decode_direct_kernel(
     float m = -INFINITY, l = 0.f, o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
-    auto attend = [&](int base, const u32x4 (&k)[U], const u32x4 (&v)[U]) {
+    auto attend = [&](int base, u32x4 (&k)[U], u32x4 (&v)[U]) {
+        if constexpr (FP4) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (min(base + u * TPI + grp, total - 1) >= s) {
+                    k[u] = fp4_octet(k[u][0], fp4_scale(k[u][1]));
+                    v[u] = fp4_octet(v[u][0], fp4_scale(v[u][1]));
+                }
+        }
         float sc[U], mx = m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -195,7 +217,11 @@ __global__ __launch_bounds__(kDirectThreads, 4) void decode_direct_kernel(
 template <int D, bool MULTI>
 static void launch_direct(const DirectArgs &a, const typename DirectPrefixes<MULTI>::type &pfx, hipStream_t stream) {
     const dim3 grid((unsigned)a.Hkv, (unsigned)a.G, (unsigned)a.n_tokens), block(kDirectThreads);
-    if constexpr (!MULTI) {                       // (no entry point appends with several prefixes)
+    if constexpr (!MULTI) {
+        if (a.fp4) {
+            hipLaunchKernelGGL((decode_direct_kernel<D, false, false, true>), grid, block, 0, stream, a, pfx);
+            return;
+        }                       // (no entry point appends with several prefixes)
         if (a.k_new) {
             hipLaunchKernelGGL((decode_direct_kernel<D, false, true>), grid, block, 0, stream, a, pfx);
             return;
@@ -208,6 +234,7 @@ hipError_t launch_decode_direct(const DirectArgs &a, const DirectOne *one, const
                                 hipStream_t stream) {
     if (a.n_tokens == 0) return hipSuccess;
     if (a.n_tokens > 65535 || (!one && !many) || (!one && a.k_new)) return hipErrorInvalidValue;
+    if (a.fp4 && (!one || a.k_new)) return hipErrorInvalidValue;           // (no entry point asks for it)
     if (head_dim == 128 && one) launch_direct<128, false>(a, *one, stream);
     else if (head_dim == 128) launch_direct<128, true>(a, *many, stream);
     else if (head_dim == 64 && one) launch_direct<64, false>(a, *one, stream);

@@ -84,6 +84,7 @@ struct DirectArgs {              // a small decode step in one launch (decode_di
     int64_t q_stride_token, q_stride_head, o_stride_token, o_stride_head, sys_stride_token, sys_stride_head;
     int64_t new_stride_token, new_stride_head;
     int n_tokens, Hq, Hkv, G, max_ctx, block_size_log2, max_blocks_per_seq, out_is_fp32;
+    int fp4;                     // the context cache holds 4-bit codes
     float scale_log2;
 };
 struct DirectOne {               // its system prompt

@@ -634,7 +634,10 @@ bool light_if_spare(int64_t sys_wgs, int64_t ctx_wgs) {
 // form (10 requests of 8 heads, contexts of 287 .. 1540, 14.8 us in two launches and 19.3 in one).
 //   Workgroups: 256 fit the machine.  As many again cost 1.3 us, and 1.8 without query groups, where two launches
 // have no less to work on at once (50 requests of 16 heads of 64, s = 42, 7.9 us in two and 10.6 in one).
-bool direct_form(const ra_params *p, int32_t total_q, int max_ctx, double sys_mean) {
+//   4-bit contexts: 17/64 of the bytes, and rows that take about twice as long to work off.  Over 120 drawn steps (1 .. 64
+// requests, contexts of 8 .. 3000) the choice takes 0.86 of the two-launch time in the mean, and more than 1.05 of it in one
+// (8.8 -> 10.0 us); with the estimate of bf16 contexts three did, up to 1.26 (10.6 -> 13.4 us).
+bool direct_form(const ra_params *p, int32_t total_q, int max_ctx, double sys_mean, bool fp4) {
     if (p->sys_chunk_tokens != 0 || p->ctx_part_tokens != 0 || total_q > 65535) return false;
     double held = (double)p->num_blocks * p->block_size;
     if (held < total_q) held = (double)total_q * max_ctx;            // (was not filled in)
@@ -642,12 +645,13 @@ bool direct_form(const ra_params *p, int32_t total_q, int max_ctx, double sys_me
     const double workgroups = (double)total_q * p->num_q_heads, row_bytes = 4.0 * p->head_dim;
     const int group = p->num_q_heads / p->num_kv_heads;
     const double tiles = ceil(total_q * (double)group / 32);
-    const double mb = (tiles * sys_mean + total_q * mean) * p->num_kv_heads * row_bytes / 1e6;
+    const double ctx_bytes = fp4 ? 17.0 / 64 : 1, ctx_rows = fp4 ? 2 : 1;
+    const double mb = (tiles * sys_mean + total_q * mean * ctx_bytes) * p->num_kv_heads * row_bytes / 1e6;
     const double round = p->head_dim == 128 ? 256 : 512, reach = longest < 1.5 * mean ? longest : 1.5 * mean;
     if (p->sys_len + reach > (reach <= 3 * round ? 6 : mb > 60 ? 5 : 4) * round) return false;
     const double rate = p->head_dim == 128 ? 300 : 460;              // rows of a workgroup per us
-    const double one = (p->sys_len + longest) / rate, even = (sys_mean + mean) / rate * workgroups / 256,
-                 moved = workgroups * (sys_mean + mean) * row_bytes / 16.8e6;
+    const double one = (p->sys_len + longest * ctx_rows) / rate, even = (sys_mean + mean * ctx_rows) / rate * workgroups / 256,
+                 moved = workgroups * (sys_mean + mean * ctx_bytes) * row_bytes / 16.8e6;
     const double most = one > even ? (one > moved ? one : moved) : (even > moved ? even : moved);
     const double direct_us = 6.5 + most + (group > 1 ? 1.3 : 1.8) * (ceil(workgroups / 256) - 1);
     const double tile_us = 9.4 + mb / 8.9 + 0.34 * log2(1 + mb) + workgroups * 0.56e-3;
@@ -767,7 +771,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
 
     // A small decode step in one launch.  (A timeline is one of the two-launch form: it is taken of the partial
     // attention, and the result is this form's all the same.)
-    const bool direct_step = !naive && !prefill && !fp4 && mask == 3 && direct_form(p, total_q, pl.max_ctx, groups.sys_len);
+    const bool direct_step = !naive && !prefill && mask == 3 && direct_form(p, total_q, pl.max_ctx, groups.sys_len, fp4);
     auto launch_direct_step = [&]() -> ra_status {
         ra::DirectArgs d{};
         d.q = static_cast<const uint16_t *>(q);
@@ -797,6 +801,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         d.block_size_log2 = pl.block_size_log2;
         d.max_blocks_per_seq = p->max_blocks_per_seq;
         d.out_is_fp32 = p->out_is_fp32;
+        d.fp4 = fp4 ? 1 : 0;
         d.scale_log2 = scale_log2;
         ra::DirectOne one{static_cast<const uint16_t *>(prefixes[0].k_sys),
                           static_cast<const uint16_t *>(prefixes[0].v_sys), prefixes[0].sys_len};
