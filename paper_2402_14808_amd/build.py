@@ -8,8 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librelayattn.so")
 SOURCES = ["relay_attn.hip", "relay_tiles.hip", "decode_direct.hip", "relay_rows.hip", "ctx_paged.hip", "fuse.hip", "validate.hip",
-           "fp4_cache.hip", "tables.hip", "cache_calls.hip"]
-HEADERS = ["ra_device.h", "ra_kernels.h", "rows_item.h", "token_place.h", "fp4.h", "fp4_attend.h", "ra_host.h",
+           "fp4_cache.hip", "fp4_direct.hip", "tables.hip", "cache_calls.hip"]
+HEADERS = ["ra_device.h", "ra_kernels.h", "rows_item.h", "token_place.h", "fp4.h", "fp4_attend.h", "ra_host.h", "direct_kernel.h",
            os.path.join("..", "..", "include", "relay_attn.h")]
 
 # -packed-fp32-ops off: scalar float code must not be fused into v_pk_*_f32 forms.

@@ -1,5 +1,5 @@
 // Host side of the calls around the 4-bit context cache and the block tables (include/relay_attn.h): argument checks before
-// any HIP call, then one launch.  (Attention over the cache shares the plans of the bf16 calls: relay_attn.hip.)
+// any HIP call, then the launches.  Attention over the cache shares the plans of the bf16 calls (relay_attn.hip).
 #include "../../include/relay_attn.h"
 
 #include <hip/hip_runtime.h>
@@ -50,6 +50,8 @@ ra_status fp4_rows(const ra_params *p, void *k, void *v, int64_t stride_token, i
                                                                                                        : RA_ERR_HIP;
 }
 
+constexpr ra::Fp4Calls kFp4Calls{ra::launch_decode_direct_fp4};
+
 }  // namespace
 
 extern "C" {
@@ -80,6 +82,27 @@ ra_status relay_attn_cache_read_fp4(const ra_params *p, void *k_out, void *v_out
     return fp4_rows(p, k_out, v_out, out_stride_token, out_stride_head, cu_seqlens_q, total_q, slot_map,
                     const_cast<void *>(k_cache), const_cast<void *>(v_cache), block_tables, context_lens, hip_stream,
                     true);
+}
+
+ra_status relay_attn_decode_fp4(const ra_params *p, const void *q, const void *k_sys, const void *v_sys,
+                                const void *k_cache, const void *v_cache, const int32_t *block_tables,
+                                const int32_t *context_lens, void *out, float *lse_out, void *workspace,
+                                size_t workspace_bytes, void *hip_stream) {
+    if (!p) return RA_ERR_INVALID_ARG;
+    return ra::attend_fp4(p, q, nullptr, p->batch, 1, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out,
+                          lse_out, workspace, workspace_bytes, hip_stream, kFp4Calls);
+}
+
+ra_status relay_attn_prefill_fp4(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, int32_t total_q,
+                                 int32_t max_q_len, const void *k_sys, const void *v_sys, const void *k_cache,
+                                 const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
+                                 void *out, float *lse_out, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream) {
+    if (!p || max_q_len < 0 || total_q < 0) return RA_ERR_INVALID_ARG;
+    if (total_q > 0 && (!cu_seqlens_q || p->batch < 1)) return RA_ERR_INVALID_ARG;
+    if ((int64_t)max_q_len * p->batch < total_q) return RA_ERR_INVALID_ARG;
+    return ra::attend_fp4(p, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables,
+                          context_lens, out, lse_out, workspace, workspace_bytes, hip_stream, kFp4Calls);
 }
 
 ra_status relay_attn_update_tables(const ra_params *p, const int32_t *old_lens, const int32_t *new_lens,

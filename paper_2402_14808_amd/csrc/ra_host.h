@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include "ra_kernels.h"
+
 namespace ra {
 
 constexpr int kFp4LeastBlock = 8;     // the 4-bit kernels take eight positions of a block at a time
@@ -35,5 +37,15 @@ inline ra_status check_params(const ra_params *p, int32_t total_q) {
     if ((int64_t)total_q * p->num_q_heads > (1 << 28)) return RA_ERR_UNSUPPORTED;
     return RA_OK;
 }
+
+// Attention over a 4-bit context cache: the plans and launches of the bf16 calls (relay_attn.hip), with the kernels
+// that those do not have handed in.  cu_seqlens_q null: a decode step.
+struct Fp4Calls {
+    hipError_t (*decode_direct)(const DirectArgs &, const DirectOne &, int head_dim, hipStream_t);
+};
+ra_status attend_fp4(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, int32_t total_q, int32_t max_q_len,
+                     const void *k_sys, const void *v_sys, const void *k_cache, const void *v_cache,
+                     const int32_t *block_tables, const int32_t *context_lens, void *out, float *lse_out,
+                     void *workspace, size_t workspace_bytes, void *hip_stream, const Fp4Calls &calls);
 
 }  // namespace ra

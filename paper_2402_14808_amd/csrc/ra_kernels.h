@@ -84,7 +84,6 @@ struct DirectArgs {              // a small decode step in one launch (decode_di
     int64_t q_stride_token, q_stride_head, o_stride_token, o_stride_head, sys_stride_token, sys_stride_head;
     int64_t new_stride_token, new_stride_head;
     int n_tokens, Hq, Hkv, G, max_ctx, block_size_log2, max_blocks_per_seq, out_is_fp32;
-    int fp4;                     // the context cache holds 4-bit codes
     float scale_log2;
 };
 struct DirectOne {               // its system prompt
@@ -182,6 +181,7 @@ hipError_t launch_relay_rows(const RowsArgs &a, int head_dim, hipStream_t stream
 hipError_t launch_relay_tiles(const TileArgs &a, int head_dim, hipStream_t stream);
 hipError_t launch_decode_direct(const DirectArgs &a, const DirectOne *one, const DirectMany *many, int head_dim,
                                 hipStream_t stream);
+hipError_t launch_decode_direct_fp4(const DirectArgs &a, const DirectOne &one, int head_dim, hipStream_t stream);
 hipError_t launch_cache_append(const AppendArgs &a, hipStream_t stream);
 hipError_t launch_fp4_rows(const Fp4RowsArgs &a, int head_dim, bool read, hipStream_t stream);
 hipError_t launch_update_tables(const TableArgs &a, hipStream_t stream);

@@ -678,9 +678,10 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
               bool naive, int32_t num_prefixes = 0, const ra_prefix *prefixes = nullptr,
               int phases = 3, const NewRows *append = nullptr,
               const int32_t *req_order = nullptr, const int32_t *req_prefix = nullptr,
-              const int32_t *prefix_num_tokens = nullptr, const Timeline *timeline = nullptr, bool fp4 = false) {
+              const int32_t *prefix_num_tokens = nullptr, const Timeline *timeline = nullptr, const ra::Fp4Calls *fp4_calls = nullptr) {
     ra_status st = check_params(p, total_q);
     if (st != RA_OK) return st;
+    const bool fp4 = fp4_calls != nullptr;
     if (fp4 && p->block_size < kFp4LeastBlock) return RA_ERR_UNSUPPORTED;
     if (naive && p->sys_len != 0) return RA_ERR_INVALID_ARG;
     if (append) {
@@ -801,10 +802,10 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         d.block_size_log2 = pl.block_size_log2;
         d.max_blocks_per_seq = p->max_blocks_per_seq;
         d.out_is_fp32 = p->out_is_fp32;
-        d.fp4 = fp4 ? 1 : 0;
         d.scale_log2 = scale_log2;
         ra::DirectOne one{static_cast<const uint16_t *>(prefixes[0].k_sys),
                           static_cast<const uint16_t *>(prefixes[0].v_sys), prefixes[0].sys_len};
+        if (fp4) return fp4_calls->decode_direct(d, one, p->head_dim, stream) == hipSuccess ? RA_OK : RA_ERR_HIP;
         ra::DirectMany many{};
         if (num_prefixes > 1) {
             many.n = num_prefixes;
@@ -1054,6 +1055,16 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
 }
 
 }  // namespace
+
+ra_status ra::attend_fp4(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, int32_t total_q,
+                         int32_t max_q_len, const void *k_sys, const void *v_sys, const void *k_cache,
+                         const void *v_cache, const int32_t *block_tables, const int32_t *context_lens, void *out,
+                         float *lse_out, void *workspace, size_t workspace_bytes, void *hip_stream,
+                         const Fp4Calls &calls) {
+    return run(p, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out,
+               lse_out, workspace, workspace_bytes, hip_stream, false, 0, nullptr, 3, nullptr, nullptr, nullptr,
+               nullptr, nullptr, &calls);
+}
 
 extern "C" {
 
@@ -1359,29 +1370,6 @@ ra_status relay_attn_cache_append(const ra_params *p, const void *k_new, const v
     if (ra::launch_cache_append(a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return RA_ERR_HIP;
     return RA_OK;
-}
-
-ra_status relay_attn_decode_fp4(const ra_params *p, const void *q, const void *k_sys, const void *v_sys,
-                                const void *k_cache, const void *v_cache, const int32_t *block_tables,
-                                const int32_t *context_lens, void *out, float *lse_out, void *workspace,
-                                size_t workspace_bytes, void *hip_stream) {
-    if (!p) return RA_ERR_INVALID_ARG;
-    return run(p, q, nullptr, p->batch, 1, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out, lse_out,
-               workspace, workspace_bytes, hip_stream, false, 0, nullptr, 3, nullptr, nullptr, nullptr, nullptr,
-               nullptr, true);
-}
-
-ra_status relay_attn_prefill_fp4(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, int32_t total_q,
-                                 int32_t max_q_len, const void *k_sys, const void *v_sys, const void *k_cache,
-                                 const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
-                                 void *out, float *lse_out, void *workspace, size_t workspace_bytes,
-                                 void *hip_stream) {
-    if (!p || max_q_len < 0 || total_q < 0) return RA_ERR_INVALID_ARG;
-    if (total_q > 0 && (!cu_seqlens_q || p->batch < 1)) return RA_ERR_INVALID_ARG;
-    if ((int64_t)max_q_len * p->batch < total_q) return RA_ERR_INVALID_ARG;
-    return run(p, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out,
-               lse_out, workspace, workspace_bytes, hip_stream, false, 0, nullptr, 3, nullptr, nullptr, nullptr,
-               nullptr, nullptr, true);
 }
 
 ra_status relay_attn_system_cache_layout(const ra_params *p, int64_t *stride_token_out,
