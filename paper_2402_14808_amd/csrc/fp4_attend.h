@@ -1,5 +1,5 @@
-// A span of one request's 4-bit context for the query heads of one kv head: the context part of a decode step, one
-// wavefront per span (Eq. 7, second term; the format: fp4.h).
+// A span of one request's 4-bit context for the query rows of one kv head: the context part of a decode step, or of a prompt
+// phase that brings few new tokens, one wavefront per span (Eq. 7, second term; the format: fp4.h).
 //
 // A tile is 32 positions.  Both products run on v_mfma_f32_16x16x32_bf16 with the values converted on the way from the
 // registers the loads landed in.  What makes that possible is that the contraction index of a
@@ -13,6 +13,8 @@
 //                 halves between two positions (v_perm_b32); product n gets channel 8 i + n.  The words come through the
 //                 wavefront's own LDS: loaded as they are needed, 4 bytes a lane, they held the loads of a launch to 5.4
 //                 TB/s (d = 128) and 4.0 (64), 16 bytes a lane to 6.2 and more.
+// A decode step has up to 8 rows, the query heads of the kv head; in the prompt phase row n is new token n / G and head n % G of
+// them, in one or two groups (CG) of 16 that share what a tile costs to load and convert.
 // The rows' powers of two are part of the conversions, so both operands are exact, and P is split into a high
 // and a low bfloat16 part as in the bf16 kernels.
 // Bound: HBM.  A tile is 4.25 KiB (d = 128) and some 200 vector instructions.
@@ -38,7 +40,9 @@ __device__ __forceinline__ float sum_with_other_row(float x) {
 
 constexpr float kFp4LazyLog2 = 8.0f;              // see kLazyLog2 in rows_item.h
 
-// Positions [key_begin, key_end) (key_begin a multiple of 32) of request `req`, kv head g, into partial `part_index`.
+// Positions [key_begin, key_end) (key_begin a multiple of 32) of request `req`, kv head g, into partial `part_index`, for its
+// rows: the packed tokens from `token0` on, the first of which sees the positions below first_end, each further one a
+// position more (a decode step: one token, and all of them).
 // `lds`: Fp4Lds<D>::BYTES bytes that belong to the wavefront, aligned to 16.
 constexpr int kFp4TableEntries = kMaxPartBlocks + 32 / 8;
 template <int D>
@@ -48,9 +52,10 @@ struct Fp4Lds {                                   // of the two tiles in turn
     static constexpr int S_TILE = 2 * Fp4<D>::GROUPS * 32;      // scales [K, V][group][position]
     static constexpr int V_AT = TABLE, S_AT = V_AT + 2 * V_TILE, BYTES = S_AT + 2 * S_TILE;
 };
-template <int D>
-__device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, const int g, const int key_begin,
-                                           int key_end, const int part_index, const int lane, unsigned char *lds) {
+template <int D, int CG>
+__device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, const int g, const int token0, const int rows,
+                                           const int first_end, const int key_begin, int key_end, const int part_index,
+                                           const int lane, unsigned char *lds) {
     constexpr int KW = D / 32;                    // code words of a lane's part of a K row; steps of S^T
     constexpr int NT = D / 16;                    // products of O^T
     constexpr int ROW = Fp4<D>::ROW;
@@ -79,16 +84,26 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
     const bool flip = a.scale_log2 < 0.f;
     const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);
     const float lazy_raw = kFp4LazyLog2 / scale;
-    bf16x8 qf[KW];
+    bf16x8 qf[CG][KW];
+    int row_end[CG], row_of[CG];                  // positions that a lane's row sees; its output row
 #pragma unroll
-    for (int n = 0; n < KW; ++n) {
-        u32x4 w = {0, 0, 0, 0};
-        if (col < a.G)
-            w = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)req * a.q_stride_token +
-                                                 (int64_t)(g * a.G + col) * a.q_stride_head + h * (D / 4) + 8 * n);
-        if (flip) w ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-        qf[n] = __builtin_bit_cast(bf16x8, w);
+    for (int c = 0; c < CG; ++c) {
+        const int n = 16 * c + col, j = CG > 1 ? n / a.G : 0;
+        const int token = token0 + j, hq = g * a.G + n - j * a.G;
+        row_end[c] = CG > 1 ? min(key_end, first_end + j) : key_end;
+        row_of[c] = n < rows ? token * a.Hq + hq : -1;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            u32x4 w = {0, 0, 0, 0};
+            if (n < rows)
+                w = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head +
+                                                     h * (D / 4) + 8 * k);
+            if (flip) w ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+            qf[c][k] = __builtin_bit_cast(bf16x8, w);
+        }
     }
+    // below this, no row misses a position
+    const int all_see = CG > 1 ? min(key_end, first_end) : key_end;
 
     // A lane loads quarter h of positions kp and kp + 4 of K and of V (eight positions that begin at a multiple of eight lie
     // in one block), and four scales: of K in the lower lanes and of V in the upper ones (d = 64 has half as many, and takes
@@ -150,19 +165,24 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         }
     };
 
-    f32x4 acc[NT];
+    f32x4 acc[CG][NT];
+    float m_run[CG], msc[CG], l_run[CG];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, msc = 0.f, l_run = 0.f;
+    for (int c = 0; c < CG; ++c) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m_run[c] = -INFINITY, msc[c] = 0.f, l_run[c] = 0.f;
+    }
 
     auto compute = [&](int tile0, const Tile (&t)[2]) {       // two tiles: their chains of products are independent
         through_lds(t);
         u32x2 v_scale[2];
-        f32x4 s[4];                               // s[2 x + u]: product u of tile x
+        f32x4 s[CG][4];                           // s[..][2 x + u]: product u of tile x
         float ks[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < CG; ++c) s[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
             // byte kp % 4 of the word to bits 23 .. 30 (the conversions read no other)
             const uint32_t word = *reinterpret_cast<const uint32_t *>(ks_get + (i / 2) * L::S_TILE + 4 * (i & 1));
             ks[i] = __uint_as_float(__builtin_amdgcn_alignbit(word, word, (8 * (col & 3) + 9) & 31));
@@ -170,56 +190,71 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
 #pragma unroll
         for (int n = 0; n < KW; ++n)              // (the four chains in turn: a product that waits for the one before it stalls)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    __builtin_bit_cast(bf16x8, fp4_octet(t[i / 2].k[i & 1][n], ks[i])), qf[n], s[i], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_octet(t[i / 2].k[i & 1][n], ks[i]));
+                s[0][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[0][n], s[0][i], 0, 0, 0);
+                if (CG > 1) s[CG - 1][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[CG - 1][n], s[CG - 1][i], 0, 0, 0);
+            }
 #pragma unroll
         for (int x = 0; x < 2; ++x) v_scale[x] = *reinterpret_cast<const u32x2 *>(vs_get + x * L::S_TILE);
-        if (tile0 + 64 > key_end) {               // ragged end: no weight and a harmless power of two behind it
+        if (tile0 + 64 > all_see) {               // no weight behind the last position that a row sees
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int mine = min(max(key_end - (tile0 + 32 * x + 8 * h), 0), 8);
+            for (int c = 0; c < CG; ++c)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int x = 0; x < 2; ++x) {
+                    const int mine = row_end[c] - (tile0 + 32 * x + 8 * h);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[2 * x + u][r] = 4 * u + r < mine ? s[2 * x + u][r] : -INFINITY;
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[c][2 * x + u][r] = 4 * u + r < mine ? s[c][2 * x + u][r] : -INFINITY;
+                }
+        }
+        if (tile0 + 64 > key_end) {               // ragged end: a harmless power of two behind it
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    const int bytes = min(max(mine - 4 * w, 0), 4);
+                    const int bytes = min(max(key_end - (tile0 + 32 * x + 8 * h) - 4 * w, 0), 4);
                     const uint32_t word = v_scale[x][w];
                     v_scale[x][w] = bytes == 4 ? word : word & ((1u << (8 * bytes)) - 1u);
                 }
-            }
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])));
         // The maximum that the sums are expressed against moves when a column outgrew it by the margin or sees its
         // first key; only then do the four lanes of a column have to agree on it.
-        if (__builtin_amdgcn_ballot_w64(mx > m_run + lazy_raw) != 0) {
-            mx = max_with_other_half(max_with_other_row(mx));
-            const float m_new = fmaxf(m_run, mx);
-            const float msc_new = m_new == -INFINITY ? 0.f : m_new * scale;
-            const float corr = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(msc - msc_new);
-            l_run *= corr;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[n] *= corr;
-            m_run = m_new;
-            msc = msc_new;
+        for (int c = 0; c < CG; ++c) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[c][i][0], s[c][i][1]), fmaxf(s[c][i][2], s[c][i][3])));
+            if (__builtin_amdgcn_ballot_w64(mx > m_run[c] + lazy_raw) != 0) {
+                mx = max_with_other_half(max_with_other_row(mx));
+                const float m_new = fmaxf(m_run[c], mx);
+                const float msc_new = m_new == -INFINITY ? 0.f : m_new * scale;
+                const float corr = m_run[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(msc[c] - msc_new);
+                l_run[c] *= corr;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[c][n] *= corr;
+                m_run[c] = m_new;
+                msc[c] = msc_new;
+            }
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            uint32_t hi[4], lo[4];
+            bf16x8 ph[CG], pl[CG];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * x + i / 2][2 * (i & 1)], scale, -msc));
-                const float p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * x + i / 2][2 * (i & 1) + 1], scale, -msc));
-                l_run += p0 + p1;
-                hi[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
-                lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - bf16_lo(hi[i]), p1 - bf16_hi(hi[i])}), bf16x2));
+            for (int c = 0; c < CG; ++c) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * x + i / 2][2 * (i & 1)], scale, -msc[c]));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * x + i / 2][2 * (i & 1) + 1], scale, -msc[c]));
+                    l_run[c] += p0 + p1;
+                    hi[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+                    lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - bf16_lo(hi[i]), p1 - bf16_hi(hi[i])}), bf16x2));
+                }
+                ph[c] = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
+                pl[c] = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
             }
-            const bf16x8 ph = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
-            const bf16x8 pl = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
             float vs[8];
             uint32_t w[8];
 #pragma unroll
@@ -239,10 +274,14 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
                     odd[p] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
                 }
                 const bf16x8 ve = __builtin_bit_cast(bf16x8, even), vo = __builtin_bit_cast(bf16x8, odd);
-                acc[2 * BYTE] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph, acc[2 * BYTE], 0, 0, 0);
-                acc[2 * BYTE + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, ph, acc[2 * BYTE + 1], 0, 0, 0);
-                acc[2 * BYTE] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl, acc[2 * BYTE], 0, 0, 0);
-                acc[2 * BYTE + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, pl, acc[2 * BYTE + 1], 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < CG; ++c) {
+                    f32x4 &e = acc[c][2 * BYTE], &o = acc[c][2 * BYTE + 1];
+                    e = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph[c], e, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, ph[c], o, 0, 0, 0);
+                    e = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl[c], e, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, pl[c], o, 0, 0, 0);
+                }
             };
             products(std::integral_constant<int, 0>{});
             products(std::integral_constant<int, 1>{});
@@ -272,10 +311,12 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         }
     }
 
-    l_run = sum_with_other_half(sum_with_other_row(l_run));
-    if (col < a.G) {
-        const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-        const int64_t prow = (int64_t)part_index * a.rows + (int64_t)req * a.Hq + g * a.G + col;
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+        const float l = sum_with_other_half(sum_with_other_row(l_run[c]));
+        if (row_of[c] < 0) continue;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int64_t prow = (int64_t)part_index * a.rows + row_of[c];
         float *dst = a.part_o + prow * D;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {             // row 4 h + r of product n is channel 8 (4 h + r) + n, see above
@@ -283,12 +324,11 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
             float *to = dst + (D == 128 ? 8 * i : 8 * (i & 7) + 4 * (i >> 3));
             // (d = 64: lanes 8 .. 15 of a group take the upper half of the words)
 #pragma unroll
-            for (int n = 0; n < NT; n += 4) {
+            for (int n = 0; n < NT; n += 4)
                 *reinterpret_cast<f32x4 *>(to + n) =
-                    f32x4{acc[n][r] * inv, acc[n + 1][r] * inv, acc[n + 2][r] * inv, acc[n + 3][r] * inv};
-            }
+                    f32x4{acc[c][n][r] * inv, acc[c][n + 1][r] * inv, acc[c][n + 2][r] * inv, acc[c][n + 3][r] * inv};
         }
-        if (h == 0) a.part_lse[prow] = l_run > 0.f ? msc + log2f(l_run) : -INFINITY;
+        if (h == 0) a.part_lse[prow] = l > 0.f ? msc[c] + log2f(l) : -INFINITY;
     }
 }
 

@@ -68,6 +68,10 @@ struct TileArgs {                // both partial attentions of a decode step in 
     int block_size_log2, max_blocks_per_seq, rows;
     int sys_head_fastest;        // system item order: kv head varies fastest (token-major cache)
     int fp4;                     // the context cache holds 4-bit codes
+    // a prompt phase of few new tokens per request (4-bit caches only; null: a decode step): request i of `batch` owns the
+    // packed tokens cu_seqlens_q[i] .., and up to 32 rows (tokens times G) of it are taken
+    const int32_t *cu_seqlens_q;
+    int batch;
     float scale_log2;
     // Measurement aid: when not null, wavefront w of the launch (4 per workgroup) stores the
     // 100 MHz counter at its begin and its end in timeline[2w], timeline[2w+1] (w < timeline_waves).

@@ -25,6 +25,7 @@ using ra::kFp4LeastBlock;
 namespace {
 
 constexpr int32_t kAbiVersion = 6;
+constexpr int kFewRows = 32;          // query rows of a request and kv head that the tile launch takes in the prompt phase
 constexpr int kWholeMinTokens = 32;   // new tokens per request, on average, from which the prompt phase is one launch
 
 struct Plan {
@@ -252,6 +253,7 @@ struct DecodeWay {
     bool by_bound = false;         // for contexts as long as the bound allows, whatever the cache holds
     bool rows_by_bound = false;    // the kind of its system items chosen so
     int64_t least_turns = 0;       // turns that a streaming system workgroup should at least have
+    int32_t contexts = 0;          // contexts, where the step's tokens share them (0: one a token)
     // (A workspace too small for the plan takes none of these refinements: they trade system chunks for context slots,
     // and some of the least workspaces that were accepted did not hold the slots, 6.1 MB of 6.6.)
 };
@@ -307,7 +309,8 @@ Plan make_plan(const ra_params *p, int32_t total_q, PlanKind kind, int32_t max_q
         const int64_t base_items = sys_base_items > 0 ? sys_base_items
                                                       : (int64_t)p->num_kv_heads * pl.n_mtiles;
         const int64_t t_max = pl.max_ctx > 0 ? ceil_div(pl.max_ctx, 32) : 0;   // tiles of one context
-        const int64_t ctx_tiles = (int64_t)total_q * p->num_kv_heads * t_max;
+        const int64_t contexts = way.contexts > 0 ? way.contexts : total_q;
+        const int64_t ctx_tiles = contexts * p->num_kv_heads * t_max;
         // What the launch is planned for: the contexts at the bound, or as many of their tiles as the cache can
         // hold where those are fewer (a num_blocks that does not even hold a token each was not filled in): a bound
         // twenty times the contexts had 7100 tiles planned for where 180 were there (18 requests of 32 heads, 3 .. 21
@@ -319,9 +322,9 @@ Plan make_plan(const ra_params *p, int32_t total_q, PlanKind kind, int32_t max_q
         int64_t ctx_like = ctx_tiles;
         if (!way.by_bound) {
             const int64_t held = (int64_t)p->num_blocks * p->block_size;
-            const int64_t tiles = p->num_kv_heads * (held / 32 + (total_q + 1) / 2);
-            const bool many_rows = pl.n_mtiles >= 4 && tiles >= 4 * (int64_t)total_q * p->num_kv_heads;
-            if (held >= total_q && tiles < ctx_like && !many_rows) ctx_like = tiles;
+            const int64_t tiles = p->num_kv_heads * (held / 32 + (contexts + 1) / 2);
+            const bool many_rows = pl.n_mtiles >= 4 && tiles >= 4 * contexts * p->num_kv_heads;
+            if (held >= contexts && tiles < ctx_like && !many_rows) ctx_like = tiles;
         }
         const int64_t all_tiles = base_items * sys_tiles + ctx_like;
         if (ctx_tiles > INT32_MAX) {
@@ -337,7 +340,7 @@ Plan make_plan(const ra_params *p, int32_t total_q, PlanKind kind, int32_t max_q
         if (t_star16 < 24) t_star16 = 24;
         const int64_t t_star = (t_star16 + 15) / 16;
         int64_t sys_wgs = 0, t_sys = 0, few_chunks = 0;
-        const double t_item = ctx_tiles > 0 ? (double)ctx_like / ((double)total_q * p->num_kv_heads) : 0;   // tiles of a context
+        const double t_item = ctx_tiles > 0 ? (double)ctx_like / ((double)contexts * p->num_kv_heads) : 0;   // tiles of a context
         // Wide grouped-query batches: with B*G stacked rows per kv head in many row tiles, every
         // 32-row streaming item would pull the system K/V of its chunk into its compute unit
         // (from L2, but what a unit can draw is capped there too: 87 us at the Llama-3-8B shape).
@@ -730,7 +733,21 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         by_prefix.sys_len += (double)prefixes[i].sys_len / num_prefixes;
     }
     Plan pl{};
+    // Few new tokens per request: their rows fit the two groups of 16 that a context wavefront of the tile launch takes, and the
+    // contexts are streamed as in a decode step, where the many-rows kernel has blocks of 128 rows that are nearly empty.
+    bool few = fp4 && cu_seqlens_q && total_q > 0 && max_q_len <= kFewRows / (p->num_q_heads / p->num_kv_heads) && p->sys_chunk_tokens == 0 && p->ctx_part_tokens == 0;
+    if (few) {
+        DecodeWay way;
+        way.contexts = p->batch;
+        Plan stream = make_plan(p, total_q, kRelayDecode, 1, 0, true, SIZE_MAX, {}, way);
+        // (a workspace of another call's size: as many slots as it holds, or the other form)
+        if (!stream.unsupported && stream.bytes > workspace_bytes)
+            stream = make_plan(p, total_q, kRelayDecode, 1, 0, true, workspace_bytes, {}, way);
+        few = !stream.unsupported && stream.bytes <= workspace_bytes;
+        if (few) pl = stream;
+    }
     for (size_t budget : {SIZE_MAX, workspace_bytes}) {
+        if (few) break;
         const Groups &shared = budget == SIZE_MAX ? groups : by_prefix;
         pl = make_plan(p, total_q, kind, max_q_len, multi ? sys_base_items : 0, true, budget, multi ? shared : Groups{});
         if (multi && kind == kRelayDecode && !pl.unsupported && pl.bytes > workspace_bytes)
@@ -917,7 +934,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
     }
     // Decode: system chunks (unless the many-rows kernel took them) and context parts in one
     // launch of the streaming tile kernel.
-    if ((mask & 1) && !naive && !prefill) {
+    if ((mask & 1) && !naive && (!prefill || few)) {
         ra::TileArgs t{};
         t.q = static_cast<const uint16_t *>(q);
         t.k_cache = static_cast<const uint16_t *>(k_cache);
@@ -991,6 +1008,8 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         t.sys_head_fastest = head_fastest;
         t.scale_log2 = scale_log2;
         t.fp4 = fp4 ? 1 : 0;
+        t.cu_seqlens_q = cu_seqlens_q;
+        t.batch = p->batch;
         if (timeline) t.timeline = timeline->entries, t.timeline_waves = timeline->waves;
         if (ra::launch_relay_tiles(t, p->head_dim, stream) != hipSuccess) return RA_ERR_HIP;
         if (direct_step) return launch_direct_step();
@@ -1083,6 +1102,13 @@ size_t relay_attn_workspace_bytes(const ra_params *p, int32_t total_q) {
     for (const bool rows_sys : {true, false}) {
         const Plan bound = make_plan(p, total_q, kRelayDecode, 1, 0, rows_sys, SIZE_MAX, {}, DecodeWay{true});
         if (!bound.unsupported && bound.bytes > most) most = bound.bytes;
+    }
+    // (and a prompt phase of few new tokens over a 4-bit cache)
+    if (total_q > p->batch && p->batch > 0 && (int64_t)total_q * (p->num_q_heads / p->num_kv_heads) <= (int64_t)kFewRows * p->batch) {
+        DecodeWay way;
+        way.contexts = p->batch;
+        const Plan few = make_plan(p, total_q, kRelayDecode, 1, 0, true, SIZE_MAX, {}, way);
+        if (!few.unsupported && few.bytes > most) most = few.bytes;
     }
     return most;
 }

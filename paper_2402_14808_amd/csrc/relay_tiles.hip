@@ -489,15 +489,22 @@ __device__ __forceinline__ int wave_inclusive_scan(int x, int lane) {
 // light wavefronts take nothing where the others can take all tiles at the floor, and all spans are
 // equal otherwise.  60 requests of 32/8 heads, s = 4096, contexts of 500 .. 2000 under a bound of 17392,
 // 64 system workgroups of 128 tiles: 87.8 us with work next to them, 72.4 without.
-template <int D, bool APPEND, bool FP4>
+//   FP4 > 0: the contexts hold 4-bit codes, and FP4 is the number of groups of 16 query rows that a wavefront takes of one: 1 in a
+// decode step; 2 in a prompt phase of few new tokens, where a request's rows are its packed tokens'.
+template <int D, bool APPEND, int FP4>
 __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned char *smem,
                                                  float (*sm_m)[32], float (*sm_l)[32],
                                                  int32_t (*sm_tbl)[kMaxPartBlocks]) {
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int w = ((int)blockIdx.x - a.n_sys_items) * kWaves + wave;
-    const int B = a.n_tokens;
-    auto len_of = [&](int r) { return r < B ? min(a.context_lens[r], a.max_ctx) : 0; };
+    constexpr bool PROMPT = FP4 > 1;
+    const int B = PROMPT ? a.batch : a.n_tokens;
+    // (a request without new tokens counts as an empty context: nothing of it is read)
+    auto len_of = [&](int r) {
+        if (PROMPT && r < B && a.cu_seqlens_q[r + 1] <= a.cu_seqlens_q[r]) return 0;
+        return r < B ? min(a.context_lens[r], a.max_ctx) : 0;
+    };
     auto tiles_of = [&](int c) { return max(1, (c + 31) >> 5); };
 
     // lengths of requests chunk_base .. chunk_base+63, one per lane, and their running tile count
@@ -671,16 +678,24 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
         asm volatile("" : "+v"(lane_here));
         // the wavefront that ends the item knows how many slots it has taken
         // (the address is computed per lane: scalar registers are what this function runs short of)
-        if (j + seg == T && slot + 1 < a.n_ctx_slots && lane_here < a.G) {
-            const int row = req * a.Hq + (g * a.G + lane_here);
+        [[maybe_unused]] int tok0 = req, rows = a.G, first_end = 0;
+        if constexpr (PROMPT) {                   // (a bound on the new tokens that is too low: the first 32 rows)
+            tok0 = a.cu_seqlens_q[req];
+            const int m = a.cu_seqlens_q[req + 1] - tok0;
+            rows = max(0, min(m * a.G, 16 * FP4));
+            first_end = a.context_lens[req] - m + 1;
+        }
+        if (j + seg == T && slot + 1 < a.n_ctx_slots && lane_here < rows) {
+            const int row = PROMPT ? (tok0 + lane_here / a.G) * a.Hq + g * a.G + lane_here % a.G
+                                   : req * a.Hq + (g * a.G + lane_here);
             int next = a.n_sys_chunks + slot + 1;
             asm volatile("" : "+v"(next));
             a.part_lse[(int64_t)next * a.rows + row] = __uint_as_float(kEndOfPartials);
         }
-        if constexpr (FP4) {
+        if constexpr (FP4 > 0) {
             static_assert(TileCfg<D>::SLICE >= Fp4Lds<D>::BYTES, "a span works in the wavefront's slice of LDS");
-            fp4_attend<D>(a, req, g, 32 * (int)j, min(c_req, 32 * (int)(j + seg)), a.n_sys_chunks + slot, lane_here,
-                          smem + wave * TileCfg<D>::SLICE);
+            fp4_attend<D, FP4>(a, req, g, tok0, rows, first_end, 32 * (int)j, min(c_req, 32 * (int)(j + seg)),
+                               a.n_sys_chunks + slot, lane_here, smem + wave * TileCfg<D>::SLICE);
         } else {
         Item it;
         it.g = g;
@@ -714,8 +729,8 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
 // B*G stacked rows per kv head are many row tiles that would each pull the whole system K/V into
 // their compute unit: what a unit can draw, from HBM or from L2, is the bound of this launch.
 // APPEND: the context wavefronts also perform the cache write of the decode step (k_new / v_new).
-// FP4: the context cache holds 4-bit codes (fp4_attend.h); the system prompt is bfloat16 as ever.
-template <int D, bool SYS_NT, bool MULTI, bool ROWS, bool APPEND, bool FP4 = false>
+// FP4 > 0: the context cache holds 4-bit codes (fp4_attend.h); the system prompt is bfloat16 as ever.
+template <int D, bool SYS_NT, bool MULTI, bool ROWS, bool APPEND, int FP4 = 0>
 __global__ __launch_bounds__(kThreads, 2) void relay_tile_kernel(const TileArgs a) {
     const unsigned long long t_begin = a.timeline ? __builtin_amdgcn_s_memrealtime() : 0ull;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * TileCfg<D>::SLICE];
@@ -785,14 +800,17 @@ hipError_t launch_relay_tiles(const TileArgs &a, int head_dim, hipStream_t strea
     if (fp4 && (append || multi)) return hipErrorInvalidValue;
 #define RA_LAUNCH(D_, NT_, MULTI_, ROWS_, APPEND_) \
     hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, MULTI_, ROWS_, APPEND_>), grid, block, 0, stream, a)
-#define RA_LAUNCH_FP4(D_, NT_, ROWS_) \
-    hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, false, ROWS_, false, true>), grid, block, 0, stream, a)
+#define RA_LAUNCH_FP4(D_, NT_, ROWS_, FP4_) \
+    hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, false, ROWS_, false, FP4_>), grid, block, 0, stream, a)
 #define RA_PICK(D_)                                                         \
     do {                                                                    \
-        if (fp4) {                                                          \
-            if (rows) RA_LAUNCH_FP4(D_, false, true);                       \
-            else if (sys_nt) RA_LAUNCH_FP4(D_, true, false);                \
-            else RA_LAUNCH_FP4(D_, false, false);                           \
+        if (fp4 && a.cu_seqlens_q) {                                        \
+            if (rows) RA_LAUNCH_FP4(D_, false, true, 2);                    \
+            else RA_LAUNCH_FP4(D_, false, false, 2);                        \
+        } else if (fp4) {                                                   \
+            if (rows) RA_LAUNCH_FP4(D_, false, true, 1);                    \
+            else if (sys_nt) RA_LAUNCH_FP4(D_, true, false, 1);             \
+            else RA_LAUNCH_FP4(D_, false, false, 1);                        \
         } else if (rows) {                                                         \
             if (append) RA_LAUNCH(D_, false, false, true, true);            \
             else RA_LAUNCH(D_, false, false, true, false);                  \

@@ -288,6 +288,41 @@ def test_prompt_phase_matches_oracle(cfg, extra):
     fc.check(prefill=True, ctx_part_tokens=128, sys_chunk_tokens=128)       # two launches whatever the size
 
 
+FEW = [
+    _cfg(batch=9, num_q_heads=32, num_kv_heads=4, q_lo=1, q_hi=4, ctx_lo=0, ctx_hi=300),          # up to 32 rows, groups of 8
+    _cfg(batch=9, num_q_heads=8, num_kv_heads=2, q_lo=1, q_hi=8, ctx_lo=20, ctx_hi=70, block_size=8),
+    _cfg(batch=40, num_q_heads=6, num_kv_heads=2, q_lo=1, q_hi=10, ctx_lo=0, ctx_hi=900, head_dim=64, sys_len=0),
+    _cfg(batch=3, num_q_heads=2, num_kv_heads=2, q_lo=17, q_hi=32, ctx_lo=0, ctx_hi=40, block_size=64),
+    _cfg(batch=70, num_q_heads=16, num_kv_heads=2, q_lo=1, q_hi=4, ctx_lo=1, ctx_hi=200, sys_len=1500, head_dim=64),
+    _cfg(batch=1, num_q_heads=8, num_kv_heads=1, q_lo=3, q_hi=3, ctx_lo=3000, ctx_hi=3000, sys_len=33, block_size=32),
+]
+
+
+@pytest.mark.parametrize("cfg", FEW, ids=[str(i) for i in range(len(FEW))])
+@pytest.mark.parametrize("fp32_out", [True, False], ids=["fp32", "bf16"])
+def test_prompt_phase_of_few_new_tokens(cfg, fp32_out):
+    _say("%s" % (cfg,))
+    fc = Fp4Case(W.make_case(cfg, 945, prefill=True, extra_context=True))
+    fc.check(prefill=True, fp32_out=fp32_out)
+    fc.check(prefill=True, fp32_out=fp32_out, max_context_len=0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("few", [True, False])
+def test_prompt_phase_with_requests_that_bring_nothing(d, few):
+    """Requests without new tokens in the middle and at both ends, contexts that end anywhere in a tile, one token or many."""
+    most = 8 if few else 21
+    counts = [0, 1, most, 0, 0, 3, 1, 7, 0]
+    lens = [40, 1, 33 + most, 0, 500, 64, 31, 7, 9]
+    cfg = _cfg(batch=len(lens), head_dim=d, num_q_heads=8, num_kv_heads=2, sys_len=45, ctx_hi=500)
+    rng = np.random.Generator(np.random.PCG64(11))
+    ctx = [[W.bf16_round(rng.standard_normal((c, 2, d), dtype=np.float32)) for c in lens] for _ in range(2)]
+    k_sys, v_sys = (W.bf16_round(rng.standard_normal((45, 2, d), dtype=np.float32)) for _ in range(2))
+    q = W.bf16_round(rng.standard_normal((sum(counts), 8, d), dtype=np.float32))
+    cu = np.cumsum([0] + counts).astype(np.int32)
+    Fp4Case(W.from_dense(cfg, q, k_sys, v_sys, *ctx, cu_seqlens_q=cu)).check(prefill=True)
+
+
 def test_an_infinity_spoils_the_results_that_see_it_and_no_other():
     """A key and a value of infinity and NaN in the middle of a prompt: rows in front of it are those of a clean cache."""
     cfg = _cfg(batch=2, q_lo=40, q_hi=40, sys_len=70)
