@@ -289,10 +289,11 @@ def test_prompt_phase_matches_oracle(cfg, extra):
 
 
 FEW = [
-    _cfg(batch=9, num_q_heads=32, num_kv_heads=4, q_lo=1, q_hi=4, ctx_lo=0, ctx_hi=300),          # up to 32 rows, groups of 8
-    _cfg(batch=9, num_q_heads=8, num_kv_heads=2, q_lo=1, q_hi=8, ctx_lo=20, ctx_hi=70, block_size=8),
+    _cfg(batch=9, num_q_heads=32, num_kv_heads=4, q_lo=1, q_hi=4, ctx_lo=0, ctx_hi=2300),         # up to 32 rows, groups of 8
+    _cfg(batch=9, num_q_heads=8, num_kv_heads=2, q_lo=1, q_hi=8, ctx_lo=1020, ctx_hi=1070, block_size=8),
+    _cfg(batch=9, num_q_heads=8, num_kv_heads=2, q_lo=1, q_hi=8, ctx_lo=20, ctx_hi=70, block_size=8),     # the other form
     _cfg(batch=40, num_q_heads=6, num_kv_heads=2, q_lo=1, q_hi=10, ctx_lo=0, ctx_hi=900, head_dim=64, sys_len=0),
-    _cfg(batch=3, num_q_heads=2, num_kv_heads=2, q_lo=17, q_hi=32, ctx_lo=0, ctx_hi=40, block_size=64),
+    _cfg(batch=3, num_q_heads=2, num_kv_heads=2, q_lo=17, q_hi=32, ctx_lo=1300, ctx_hi=1400, block_size=64),
     _cfg(batch=70, num_q_heads=16, num_kv_heads=2, q_lo=1, q_hi=4, ctx_lo=1, ctx_hi=200, sys_len=1500, head_dim=64),
     _cfg(batch=1, num_q_heads=8, num_kv_heads=1, q_lo=3, q_hi=3, ctx_lo=3000, ctx_hi=3000, sys_len=33, block_size=32),
 ]
@@ -304,6 +305,9 @@ def test_prompt_phase_of_few_new_tokens(cfg, fp32_out):
     _say("%s" % (cfg,))
     fc = Fp4Case(W.make_case(cfg, 945, prefill=True, extra_context=True))
     fc.check(prefill=True, fp32_out=fp32_out)
+    wide = np.full((cfg.batch, 400), W.POISON_BLOCK, dtype=np.int32)     # a loose bound
+    wide[:, :fc.case.block_tables.shape[1]] = fc.case.block_tables
+    fc.tables = _i32(wide)
     fc.check(prefill=True, fp32_out=fp32_out, max_context_len=0)
 
 
@@ -313,7 +317,7 @@ def test_prompt_phase_with_requests_that_bring_nothing(d, few):
     """Requests without new tokens in the middle and at both ends, contexts that end anywhere in a tile, one token or many."""
     most = 8 if few else 21
     counts = [0, 1, most, 0, 0, 3, 1, 7, 0]
-    lens = [40, 1, 33 + most, 0, 500, 64, 31, 7, 9]
+    lens = [40, 1, 33 + most, 0, 500, 64, 31, 7, 9000]          # (the last makes the contexts long in the mean)
     cfg = _cfg(batch=len(lens), head_dim=d, num_q_heads=8, num_kv_heads=2, sys_len=45, ctx_hi=500)
     rng = np.random.Generator(np.random.PCG64(11))
     ctx = [[W.bf16_round(rng.standard_normal((c, 2, d), dtype=np.float32)) for c in lens] for _ in range(2)]
