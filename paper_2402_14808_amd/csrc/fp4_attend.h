@@ -114,11 +114,9 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
     const int sl = D == 128 ? lane : lane & 31;   // scales: cache, group, positions 4 (sl % 8) ..
     const int s_group = (sl >> 3) & (Fp4<D>::GROUPS - 1), s_pos = 4 * (sl & 7);
     const bool s_is_v = sl >= 8 * Fp4<D>::GROUPS;
-    const int64_t lane_at = (kp & bmask) * ROW + h * (KW * 4);
-    const uint8_t *k_codes = reinterpret_cast<const uint8_t *>(a.k_cache) + lane_at;
-    const uint8_t *v_codes = reinterpret_cast<const uint8_t *>(a.v_cache) + lane_at;
-    const uint8_t *scale_bytes = reinterpret_cast<const uint8_t *>(s_is_v ? a.v_cache : a.k_cache) + scales_at +
-                                 (s_group << bsl) + (s_pos & bmask);
+    const int lane_at = (kp & bmask) * ROW + h * (KW * 4), lane_scales_at = (s_group << bsl) + (s_pos & bmask);
+    const uint8_t *k_codes = reinterpret_cast<const uint8_t *>(a.k_cache), *v_codes = reinterpret_cast<const uint8_t *>(a.v_cache);
+    const uint8_t *scale_bytes = (s_is_v ? v_codes : k_codes) + scales_at;
     const int64_t *code_tbl = tbl + (kp >> bsl), *scale_tbl = tbl + (s_pos >> bsl);
     uint32_t *const s_put = reinterpret_cast<uint32_t *>(lds + L::S_AT + 4 * sl);
     unsigned char *const v_put = lds + L::V_AT + kp * ROW + (kp >> 3) * ROW + h * (KW * 4);
@@ -142,9 +140,12 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         }
     };
     auto load = [&](int tile0, Tile &t) {
-        tile0 = min(tile0, last_tile);            // (as many loads each time: the waits count them)
+        // As many loads each time: the waits count them.  Behind the last tile all lanes take the same few bytes of it (as
+        // a whole tile, up to four of those a span were fetched again, non-temporal as they are).
+        const int none = tile0 > last_tile ? 0 : -1;
+        tile0 = min(tile0, last_tile);
         const int blk = (tile0 >> bsl) - first_blk, off = tile0 & bmask;
-        const int64_t at = code_tbl[blk] + off * ROW, scales_of = scale_tbl[blk] + off;
+        const int64_t at = code_tbl[blk] + (off * ROW + (lane_at & none)), scales_of = scale_tbl[blk] + (off + (lane_scales_at & none));
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             load_words(k_codes + at + 4 * u * ROW, t.k[u]);
