@@ -50,7 +50,8 @@ struct Fp4Lds {                                   // of the two tiles in turn
     static constexpr int TABLE = kFp4TableEntries * 8;
     static constexpr int V_TILE = 36 * Fp4<D>::ROW;             // rows, each eight of them one row further: no bank conflicts
     static constexpr int S_TILE = 2 * Fp4<D>::GROUPS * 32;      // scales [K, V][group][position]
-    static constexpr int V_AT = TABLE, S_AT = V_AT + 2 * V_TILE, BYTES = S_AT + 2 * S_TILE;
+    static constexpr int V_AT = TABLE, S_AT = V_AT + 2 * V_TILE;
+    static constexpr int K_AT = S_AT + 2 * S_TILE, BYTES = K_AT + (D == 64 ? 2 * V_TILE : 0);   // K rows, d = 64
 };
 template <int D, int CG>
 __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, const int g, const int token0, const int rows,
@@ -105,40 +106,34 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
     // below this, no row misses a position
     const int all_see = CG > 1 ? min(key_end, first_end) : key_end;
 
-    // A lane loads quarter h of positions kp and kp + 4 of K and of V (eight positions that begin at a multiple of eight lie
-    // in one block), and four scales: of K in the lower lanes and of V in the upper ones (d = 64 has half as many, and takes
-    // them twice).  Rows behind the end are loaded like the others, whatever they hold: scores and powers of two
-    // are put right below.
+    // d = 128: a lane loads quarter h of positions kp and kp + 4 of K, which it multiplies, and of V.  d = 64: half of position
+    // lane / 2 of each, 16 bytes as well, and K takes the way through LDS too (a quarter each, 8 bytes a lane, held the loads of a
+    // launch to 5.2 TB/s).  Eight positions that begin at a multiple of eight lie in one block.  Then four scales: of K in the
+    // lower lanes and of V in the upper ones (d = 64 has half as many, and takes them twice).  Rows behind the end are loaded
+    // like the others, whatever they hold: scores and powers of two are put right below.
     const int oct = D == 128 ? col : col & 7;     // V: the word of a row that this lane multiplies
     const int kp = 8 * (col >> 2) + (col & 3);
+    const int lp = D == 128 ? kp : lane >> 1, lq = D == 128 ? h : lane & 1;      // position and 16 bytes of it that this lane loads
     const int sl = D == 128 ? lane : lane & 31;   // scales: cache, group, positions 4 (sl % 8) ..
     const int s_group = (sl >> 3) & (Fp4<D>::GROUPS - 1), s_pos = 4 * (sl & 7);
     const bool s_is_v = sl >= 8 * Fp4<D>::GROUPS;
-    const int lane_at = (kp & bmask) * ROW + h * (KW * 4), lane_scales_at = (s_group << bsl) + (s_pos & bmask);
+    const int lane_at = (lp & bmask) * ROW + lq * 16, lane_scales_at = (s_group << bsl) + (s_pos & bmask);
     const uint8_t *k_codes = reinterpret_cast<const uint8_t *>(a.k_cache), *v_codes = reinterpret_cast<const uint8_t *>(a.v_cache);
     const uint8_t *scale_bytes = (s_is_v ? v_codes : k_codes) + scales_at;
-    const int64_t *code_tbl = tbl + (kp >> bsl), *scale_tbl = tbl + (s_pos >> bsl);
+    const int64_t *code_tbl = tbl + (lp >> bsl), *scale_tbl = tbl + (s_pos >> bsl);
     uint32_t *const s_put = reinterpret_cast<uint32_t *>(lds + L::S_AT + 4 * sl);
-    unsigned char *const v_put = lds + L::V_AT + kp * ROW + (kp >> 3) * ROW + h * (KW * 4);
+    unsigned char *const v_put = lds + L::V_AT + lp * ROW + (lp >> 3) * ROW + lq * 16;
     const unsigned char *const v_get = lds + L::V_AT + 9 * h * ROW + oct * 4;
+    [[maybe_unused]] const unsigned char *const k_get = lds + L::K_AT + kp * ROW + (kp >> 3) * ROW + h * 8;
     const unsigned char *const ks_get = lds + L::S_AT + (h * (D / 4) / 32) * 32 + (kp & ~7);
     const unsigned char *const vs_get = lds + L::S_AT + (Fp4<D>::GROUPS + oct / 4) * 32 + 8 * h;
 
+    constexpr int LOADS = D / 64;                 // of K, and of V, a tile
     struct Tile {
-        uint32_t k[2][KW], v[2][KW], scales;
+        u32x4 k[LOADS], v[LOADS];
+        uint32_t scales;
     };
     const int last_tile = key_begin + ((key_end - key_begin - 1) & ~31);
-    auto load_words = [](const uint8_t *from, uint32_t (&w)[KW]) {       // (rows are read once: non-temporal)
-        if constexpr (KW == 4) {
-            const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from));
-#pragma unroll
-            for (int n = 0; n < KW; ++n) w[n] = x[n];
-        } else {
-            const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(from));
-#pragma unroll
-            for (int n = 0; n < KW; ++n) w[n] = x[n];
-        }
-    };
     auto load = [&](int tile0, Tile &t) {
         // As many loads each time: the waits count them.  Behind the last tile all lanes take the same few bytes of it (as
         // a whole tile, up to four of those a span were fetched again, non-temporal as they are).
@@ -147,9 +142,9 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         const int blk = (tile0 >> bsl) - first_blk, off = tile0 & bmask;
         const int64_t at = code_tbl[blk] + (off * ROW + (lane_at & none)), scales_of = scale_tbl[blk] + (off + (lane_scales_at & none));
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            load_words(k_codes + at + 4 * u * ROW, t.k[u]);
-            load_words(v_codes + at + 4 * u * ROW, t.v[u]);
+        for (int u = 0; u < LOADS; ++u) {         // (rows are read once: non-temporal)
+            t.k[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(k_codes + at + 4 * u * ROW));
+            t.v[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v_codes + at + 4 * u * ROW));
         }
         t.scales = *reinterpret_cast<const uint32_t *>(scale_bytes + scales_of);
     };
@@ -157,12 +152,19 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             s_put[x * (L::S_TILE / 4)] = t[x].scales;
+            if constexpr (D == 64) *reinterpret_cast<u32x4 *>(v_put + (L::K_AT - L::V_AT) + x * L::V_TILE) = t[x].k[0];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                unsigned char *to = v_put + x * L::V_TILE + 4 * u * ROW;
-                if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(to) = u32x4{t[x].v[u][0], t[x].v[u][1], t[x].v[u][2], t[x].v[u][3]};
-                else *reinterpret_cast<u32x2 *>(to) = u32x2{t[x].v[u][0], t[x].v[u][1]};
-            }
+            for (int u = 0; u < LOADS; ++u) *reinterpret_cast<u32x4 *>(v_put + x * L::V_TILE + 4 * u * ROW) = t[x].v[u];
+        }
+    };
+    auto k_words = [&](const Tile (&t)[2], int i, uint32_t (&w)[KW]) {   // of product i % 2 of tile i / 2
+        if constexpr (D == 64) {
+            const u32x2 x = *reinterpret_cast<const u32x2 *>(k_get + (i / 2) * L::V_TILE + 4 * (i & 1) * ROW);
+#pragma unroll
+            for (int n = 0; n < KW; ++n) w[n] = x[n];
+        } else {
+#pragma unroll
+            for (int n = 0; n < KW; ++n) w[n] = t[i / 2].k[(i & 1) & (LOADS - 1)][n];
         }
     };
 
@@ -180,8 +182,10 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         u32x2 v_scale[2];
         f32x4 s[CG][4];                           // s[..][2 x + u]: product u of tile x
         float ks[4];
+        uint32_t kw[4][KW];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            k_words(t, i, kw[i]);
 #pragma unroll
             for (int c = 0; c < CG; ++c) s[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
             // byte kp % 4 of the word to bits 23 .. 30 (the conversions read no other)
@@ -192,7 +196,7 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         for (int n = 0; n < KW; ++n)              // (the four chains in turn: a product that waits for the one before it stalls)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_octet(t[i / 2].k[i & 1][n], ks[i]));
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_octet(kw[i][n], ks[i]));
                 s[0][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[0][n], s[0][i], 0, 0, 0);
                 if (CG > 1) s[CG - 1][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[CG - 1][n], s[CG - 1][i], 0, 0, 0);
             }

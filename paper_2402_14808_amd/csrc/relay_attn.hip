@@ -998,8 +998,9 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         // Workgroups i and i + 256 of a 512-workgroup grid share a compute unit: the context
         // workgroups 256 .. 256 + n_sys - 1 sit next to a system workgroup.
         // (A system tile holds a unit up as long as about three tiles of a 4-bit context, which are 0.27 of its bytes: 64
-        // requests of 40 heads, 300 .. 2500 behind 1024, 108.9 us counted as one, 105.6 as two, 101.7 as three, 106 as five.)
-        const int ctx_per_sys_tile = fp4 ? 3 : 1;
+        // requests of 40 heads, 300 .. 2500 behind 1024, 108.9 us counted as one, 105.6 as two, 101.7 as three, 106 as five.  With
+        // two groups of rows a context tile takes as long: 32 requests of 2 .. 8 tokens, 26.0 us counted as one, 30.9 as three.)
+        const int ctx_per_sys_tile = fp4 && !prefill ? 3 : 1;
         if (pl.paired && items + pl.ctx_wgs == kWorkgroupSlots && items <= kWorkgroupSlots / 2) {
             t.ctx_light_begin = (kWorkgroupSlots / 2 - items) * 4;
             t.ctx_light_waves = items * 4;
