@@ -15,8 +15,9 @@
 //                 TB/s (d = 128) and 4.0 (64), 16 bytes a lane to 6.2 and more.
 // A decode step has up to 8 rows, the query heads of the kv head; in the prompt phase row n is new token n / G and head n % G of
 // them, in one or two groups (CG) of 16 that share what a tile costs to load and convert.
-// The rows' powers of two are part of the conversions, so both operands are exact, and P is split into a high
-// and a low bfloat16 part as in the bf16 kernels.
+// The rows' powers of two are part of the conversions, so both operands are exact.  P is split into a high and a low bfloat16
+// part as in the bf16 kernels, 2^-17 of a weight, and for an fp32 output (EX) into three, so that what is left, 2^-26, is below
+// the sums' own rounding.
 // Bound: HBM.  A tile is 4.25 KiB (d = 128) and some 200 vector instructions.
 #pragma once
 #include "fp4.h"
@@ -53,7 +54,7 @@ struct Fp4Lds {                                   // of the two tiles in turn
     static constexpr int V_AT = TABLE, S_AT = V_AT + 2 * V_TILE;
     static constexpr int K_AT = S_AT + 2 * S_TILE, BYTES = K_AT + (D == 64 ? 2 * V_TILE : 0);   // K rows, d = 64
 };
-template <int D, int CG>
+template <int D, int CG, bool EX>
 __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, const int g, const int token0, const int rows,
                                            const int first_end, const int key_begin, int key_end, const int part_index,
                                            const int lane, unsigned char *lds) {
@@ -245,18 +246,22 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            bf16x8 ph[CG], pl[CG];
+            bf16x8 ph[CG], pl[CG], pt[CG];
 #pragma unroll
             for (int c = 0; c < CG; ++c) {
-                uint32_t hi[4], lo[4];
+                uint32_t hi[4], lo[4], third[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float p0 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * x + i / 2][2 * (i & 1)], scale, -msc[c]));
                     const float p1 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * x + i / 2][2 * (i & 1) + 1], scale, -msc[c]));
                     l_run[c] += p0 + p1;
                     hi[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
-                    lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - bf16_lo(hi[i]), p1 - bf16_hi(hi[i])}), bf16x2));
+                    const float r0 = p0 - bf16_lo(hi[i]), r1 = p1 - bf16_hi(hi[i]);
+                    lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{r0, r1}), bf16x2));
+                    if constexpr (EX)
+                        third[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{r0 - bf16_lo(lo[i]), r1 - bf16_hi(lo[i])}), bf16x2));
                 }
+                if constexpr (EX) pt[c] = __builtin_bit_cast(bf16x8, (u32x4{third[0], third[1], third[2], third[3]}));
                 ph[c] = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
                 pl[c] = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
             }
@@ -286,6 +291,10 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
                     o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, ph[c], o, 0, 0, 0);
                     e = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl[c], e, 0, 0, 0);
                     o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, pl[c], o, 0, 0, 0);
+                    if constexpr (EX) {
+                        e = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pt[c], e, 0, 0, 0);
+                        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vo, pt[c], o, 0, 0, 0);
+                    }
                 }
             };
             products(std::integral_constant<int, 0>{});

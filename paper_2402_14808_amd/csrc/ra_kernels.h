@@ -68,6 +68,7 @@ struct TileArgs {                // both partial attentions of a decode step in 
     int block_size_log2, max_blocks_per_seq, rows;
     int sys_head_fastest;        // system item order: kv head varies fastest (token-major cache)
     int fp4;                     // the context cache holds 4-bit codes
+    int exact;                   // (of a 4-bit call) weights in three bfloat16 parts, for an fp32 output
     // a prompt phase of few new tokens per request (4-bit caches only; null: a decode step): request i of `batch` owns the
     // packed tokens cu_seqlens_q[i] .., and up to 32 rows (tokens times G) of it are taken
     const int32_t *cu_seqlens_q;
@@ -121,6 +122,7 @@ struct RowsArgs {                // many query rows per kv head: prompt phase, w
     int ctx_part, n_ctx_parts, n_ctx_rowblocks, n_ctx_items;
     int block_size_log2, max_blocks_per_seq, rows, sys_head_fastest;
     int fp4;                     // the context cache holds 4-bit codes
+    int exact;                   // (of a 4-bit call) weights in three bfloat16 parts, for an fp32 output
     float scale_log2;
     // Several shared prefixes in the prompt phase (0 or 1: the fields above describe the only
     // one): prefix p owns the packed tokens pfx_tok0[p] .. +pfx_ntok[p]-1 (its requests are

@@ -892,6 +892,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         r.sys_head_fastest = head_fastest;
         r.scale_log2 = scale_log2;
         r.fp4 = fp4 ? 1 : 0;
+        r.exact = fp4 && p->out_is_fp32 ? 1 : 0;
         r.n_prefixes = num_prefixes;
         r.batch = p->batch;
         r.whole = whole ? 1 : 0;
@@ -1024,6 +1025,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         t.sys_head_fastest = head_fastest;
         t.scale_log2 = scale_log2;
         t.fp4 = fp4 ? 1 : 0;
+        t.exact = fp4 && p->out_is_fp32 ? 1 : 0;
         t.cu_seqlens_q = cu_seqlens_q;
         t.batch = p->batch;
         if (timeline) t.timeline = timeline->entries, t.timeline_waves = timeline->waves;

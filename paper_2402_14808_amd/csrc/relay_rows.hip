@@ -28,12 +28,12 @@
 
 namespace ra {
 
-template <int D, bool MULTI, bool WHOLE, bool FP4 = false>
+template <int D, bool MULTI, bool WHOLE, bool FP4 = false, bool EX = false>
 __global__ __launch_bounds__(kThreads, 2) void relay_rows_kernel(const RowsArgs a) {
     const unsigned long long t_begin = a.timeline ? __builtin_amdgcn_s_memrealtime() : 0ull;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * 2 * 64 * D * 2];
     __shared__ int32_t sm_tbl[kMaxPartBlocks];
-    rows_item<D, false, MULTI, WHOLE, FP4>(a, (int)blockIdx.x, lds, sm_tbl);
+    rows_item<D, false, MULTI, WHOLE, FP4, EX>(a, (int)blockIdx.x, lds, sm_tbl);
     if (a.timeline) {
         const unsigned w = blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
         if (threadIdx.x % kWave == 0 && w < (unsigned)a.timeline_waves) {
@@ -53,12 +53,14 @@ hipError_t launch_relay_rows(const RowsArgs &a, int head_dim, hipStream_t stream
     const dim3 grid((unsigned)groups), block(kThreads);
 #define RA_ROWS(D_, MULTI_, WHOLE_) \
     hipLaunchKernelGGL((relay_rows_kernel<D_, MULTI_, WHOLE_>), grid, block, 0, stream, a)
-#define RA_ROWS_FP4(D_, WHOLE_) \
-    hipLaunchKernelGGL((relay_rows_kernel<D_, false, WHOLE_, true>), grid, block, 0, stream, a)
+#define RA_ROWS_FP4(D_, WHOLE_, EX_) \
+    hipLaunchKernelGGL((relay_rows_kernel<D_, false, WHOLE_, true, EX_>), grid, block, 0, stream, a)
 #define RA_ROWS_D(D_)                               \
     do {                                            \
-        if (a.fp4 && a.whole) RA_ROWS_FP4(D_, true);     \
-        else if (a.fp4) RA_ROWS_FP4(D_, false);     \
+        if (a.fp4 && a.whole && a.exact) RA_ROWS_FP4(D_, true, true);   \
+        else if (a.fp4 && a.whole) RA_ROWS_FP4(D_, true, false);        \
+        else if (a.fp4 && a.exact) RA_ROWS_FP4(D_, false, true);        \
+        else if (a.fp4) RA_ROWS_FP4(D_, false, false);                  \
         else if (a.whole && multi) RA_ROWS(D_, true, true);   \
         else if (a.whole) RA_ROWS(D_, false, true); \
         else if (multi) RA_ROWS(D_, true, false);   \

@@ -88,7 +88,8 @@ struct Item {
     const uint16_t *k, *v;    // system item: K/V of kv head g (context items use the paged cache)
 };
 
-template <int D, bool SYS, bool NT, bool APPEND = false>
+// EX: P in three bfloat16 parts instead of two (see fp4_attend.h).
+template <int D, bool SYS, bool NT, bool APPEND = false, bool EX = false>
 __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const int lane,
                                        unsigned char *smem, float (*sm_m)[32], float (*sm_l)[32],
                                        int32_t (*sm_tbl)[kMaxPartBlocks]) {
@@ -299,6 +300,7 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
         // MFMA passes.  The row sum uses the unrounded fp32 weights.
         float psum = 0.f;
         uint32_t pw[8], pw_lo[8];
+        [[maybe_unused]] uint32_t pw_third[8];
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
             const float p0 = fast_exp2(s[r] - m_run), p1 = fast_exp2(s[r + 1] - m_run);
@@ -306,6 +308,10 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
             const uint32_t h = pack_bf16_hw(p0, p1);
             pw[r / 2] = h;
             pw_lo[r / 2] = pack_bf16_hw(p0 - bf16_lo(h), p1 - bf16_hi(h));
+            if constexpr (EX) {
+                const uint32_t l = pw_lo[r / 2];
+                pw_third[r / 2] = pack_bf16_hw(p0 - bf16_lo(h) - bf16_lo(l), p1 - bf16_hi(h) - bf16_hi(l));
+            }
         }
         l_run += psum;
 
@@ -333,6 +339,10 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
                 const bf16x8 vf = __builtin_bit_cast(bf16x8, v8);
                 acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, acc_o[db], 0, 0, 0);
                 acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf_lo, acc_o[db], 0, 0, 0);
+                if constexpr (EX) {
+                    const u32x4 pt = u32x4{pw_third[4 * kstep], pw_third[4 * kstep + 1], pw_third[4 * kstep + 2], pw_third[4 * kstep + 3]};
+                    acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pt), acc_o[db], 0, 0, 0);
+                }
             }
         }
         // every V operand of this tile has been read: the next tile's V takes its place
@@ -418,7 +428,7 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
 }
 
 // System workgroup: decode the grid index into (prefix, kv head, row tile, chunk).
-template <int D, bool NT, bool MULTI>
+template <int D, bool NT, bool MULTI, bool EX>
 __device__ __forceinline__ void run_system_item(const TileArgs &a, unsigned char *smem,
                                                 float (*sm_m)[32], float (*sm_l)[32],
                                                 int32_t (*sm_tbl)[kMaxPartBlocks]) {
@@ -457,7 +467,7 @@ __device__ __forceinline__ void run_system_item(const TileArgs &a, unsigned char
     it.ncols = min(32, a.pfx_tokens[pfx] * a.G - it.mt * 32);
     it.k = a.pfx_k[pfx] + (int64_t)it.g * a.sys_stride_head;
     it.v = a.pfx_v[pfx] + (int64_t)it.g * a.sys_stride_head;
-    attend<D, true, NT>(a, it, threadIdx.x & (kWave - 1), smem, sm_m, sm_l, sm_tbl);
+    attend<D, true, NT, false, EX>(a, it, threadIdx.x & (kWave - 1), smem, sm_m, sm_l, sm_tbl);
 }
 
 __device__ __forceinline__ int wave_inclusive_scan(int x, int lane) {
@@ -491,7 +501,7 @@ __device__ __forceinline__ int wave_inclusive_scan(int x, int lane) {
 // 64 system workgroups of 128 tiles: 87.8 us with work next to them, 72.4 without.
 //   FP4 > 0: the contexts hold 4-bit codes, and FP4 is the number of groups of 16 query rows that a wavefront takes of one: 1 in a
 // decode step; 2 in a prompt phase of few new tokens, where a request's rows are its packed tokens'.
-template <int D, bool APPEND, int FP4>
+template <int D, bool APPEND, int FP4, bool EX>
 __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned char *smem,
                                                  float (*sm_m)[32], float (*sm_l)[32],
                                                  int32_t (*sm_tbl)[kMaxPartBlocks]) {
@@ -694,7 +704,7 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
         }
         if constexpr (FP4 > 0) {
             static_assert(TileCfg<D>::SLICE >= Fp4Lds<D>::BYTES, "a span works in the wavefront's slice of LDS");
-            fp4_attend<D, FP4>(a, req, g, tok0, rows, first_end, 32 * (int)j, min(c_req, 32 * (int)(j + seg)),
+            fp4_attend<D, FP4, EX>(a, req, g, tok0, rows, first_end, 32 * (int)j, min(c_req, 32 * (int)(j + seg)),
                                a.n_sys_chunks + slot, lane_here, smem + wave * TileCfg<D>::SLICE);
         } else {
         Item it;
@@ -729,8 +739,8 @@ __device__ __forceinline__ void run_context_wave(const TileArgs &a, unsigned cha
 // B*G stacked rows per kv head are many row tiles that would each pull the whole system K/V into
 // their compute unit: what a unit can draw, from HBM or from L2, is the bound of this launch.
 // APPEND: the context wavefronts also perform the cache write of the decode step (k_new / v_new).
-// FP4 > 0: the context cache holds 4-bit codes (fp4_attend.h); the system prompt is bfloat16 as ever.
-template <int D, bool SYS_NT, bool MULTI, bool ROWS, bool APPEND, int FP4 = 0>
+// FP4 > 0: the context cache holds 4-bit codes (fp4_attend.h); the system prompt is bfloat16 as ever.  EX: for an fp32 output.
+template <int D, bool SYS_NT, bool MULTI, bool ROWS, bool APPEND, int FP4 = 0, bool EX = false>
 __global__ __launch_bounds__(kThreads, 2) void relay_tile_kernel(const TileArgs a) {
     const unsigned long long t_begin = a.timeline ? __builtin_amdgcn_s_memrealtime() : 0ull;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * TileCfg<D>::SLICE];
@@ -762,9 +772,9 @@ __global__ __launch_bounds__(kThreads, 2) void relay_tile_kernel(const TileArgs 
             r.rows = a.rows;
             r.sys_head_fastest = a.sys_head_fastest;
             r.scale_log2 = a.scale_log2;
-            rows_item<D, true>(r, (int)blockIdx.x, smem, &sm_tbl[0][0]);
+            rows_item<D, true, false, false, false, EX>(r, (int)blockIdx.x, smem, &sm_tbl[0][0]);
         } else {
-            run_system_item<D, SYS_NT, MULTI>(a, smem, sm_m, sm_l, sm_tbl);
+            run_system_item<D, SYS_NT, MULTI, EX>(a, smem, sm_m, sm_l, sm_tbl);
         }
     } else {
         // Context wavefronts issue in short bursts between long waits for memory; at a raised
@@ -773,7 +783,7 @@ __global__ __launch_bounds__(kThreads, 2) void relay_tile_kernel(const TileArgs 
         // through (grouped-query shape with many-rows system items 75 -> 71 us, Llama-30B shape at
         // a 2048-position prompt 34.2 -> 33.4 us).
         __builtin_amdgcn_s_setprio(3);
-        run_context_wave<D, APPEND, FP4>(a, smem, sm_m, sm_l, sm_tbl);
+        run_context_wave<D, APPEND, FP4, EX>(a, smem, sm_m, sm_l, sm_tbl);
     }
     if (a.timeline) {
         const unsigned w = blockIdx.x * kWaves + threadIdx.x / kWave;
@@ -798,19 +808,25 @@ hipError_t launch_relay_tiles(const TileArgs &a, int head_dim, hipStream_t strea
     if (rows && multi) return hipErrorInvalidValue;
     const bool fp4 = a.fp4 != 0;
     if (fp4 && (append || multi)) return hipErrorInvalidValue;
+    const bool exact = a.exact != 0;
 #define RA_LAUNCH(D_, NT_, MULTI_, ROWS_, APPEND_) \
     hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, MULTI_, ROWS_, APPEND_>), grid, block, 0, stream, a)
-#define RA_LAUNCH_FP4(D_, NT_, ROWS_, FP4_) \
-    hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, false, ROWS_, false, FP4_>), grid, block, 0, stream, a)
+#define RA_LAUNCH_FP4(D_, NT_, ROWS_, FP4_, EX_) \
+    hipLaunchKernelGGL((relay_tile_kernel<D_, NT_, false, ROWS_, false, FP4_, EX_>), grid, block, 0, stream, a)
 #define RA_PICK(D_)                                                         \
     do {                                                                    \
         if (fp4 && a.cu_seqlens_q) {                                        \
-            if (rows) RA_LAUNCH_FP4(D_, false, true, 2);                    \
-            else RA_LAUNCH_FP4(D_, false, false, 2);                        \
+            if (rows && exact) RA_LAUNCH_FP4(D_, false, true, 2, true);     \
+            else if (rows) RA_LAUNCH_FP4(D_, false, true, 2, false);        \
+            else if (exact) RA_LAUNCH_FP4(D_, false, false, 2, true);       \
+            else RA_LAUNCH_FP4(D_, false, false, 2, false);                 \
         } else if (fp4) {                                                   \
-            if (rows) RA_LAUNCH_FP4(D_, false, true, 1);                    \
-            else if (sys_nt) RA_LAUNCH_FP4(D_, true, false, 1);             \
-            else RA_LAUNCH_FP4(D_, false, false, 1);                        \
+            if (rows && exact) RA_LAUNCH_FP4(D_, false, true, 1, true);     \
+            else if (rows) RA_LAUNCH_FP4(D_, false, true, 1, false);        \
+            else if (exact && sys_nt) RA_LAUNCH_FP4(D_, true, false, 1, true); \
+            else if (exact) RA_LAUNCH_FP4(D_, false, false, 1, true);       \
+            else if (sys_nt) RA_LAUNCH_FP4(D_, true, false, 1, false);      \
+            else RA_LAUNCH_FP4(D_, false, false, 1, false);                 \
         } else if (rows) {                                                         \
             if (append) RA_LAUNCH(D_, false, false, true, true);            \
             else RA_LAUNCH(D_, false, false, true, false);                  \

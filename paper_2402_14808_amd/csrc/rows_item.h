@@ -49,7 +49,9 @@ constexpr float kLazyLog2 = 8.0f;
 // FP4: the context cache holds 4-bit codes.  The system prompt's steps are loaded as ever; a context step's codes land in
 // registers while the step before is worked off and go to the other buffer as bfloat16 (exactly, see fp4.h) when it
 // is done, in the same places.
-template <int D, bool SYS_ONLY, bool MULTI = false, bool WHOLE = false, bool FP4 = false>
+// EX: the weights in three bfloat16 parts instead of two (see fp4_attend.h); a tile's weights are made right before its products
+// then, as six sets of them would not fit the registers.
+template <int D, bool SYS_ONLY, bool MULTI = false, bool WHOLE = false, bool FP4 = false, bool EX = false>
 __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, unsigned char *lds,
                                           int32_t *sm_tbl) {
     constexpr int ROW_BYTES = D * 2;
@@ -409,6 +411,7 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
                 }
             };
             // weights of one tile, their sum, and their bf16 high + low parts (see relay_tiles.hip)
+            [[maybe_unused]] uint32_t third[8];
             auto weights = [&](const f32x16 &sc, uint32_t (&pw)[8], uint32_t (&pw_lo)[8]) {
                 const float neg_msc = -msc;
                 float psum = 0.f;
@@ -419,6 +422,10 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
                     const uint32_t h = rows_pack_bf16(p0, p1);
                     pw[r / 2] = h;
                     pw_lo[r / 2] = rows_pack_bf16(p0 - bf16_lo(h), p1 - bf16_hi(h));
+                    if constexpr (EX) {
+                        const uint32_t l = pw_lo[r / 2];
+                        third[r / 2] = rows_pack_bf16(p0 - bf16_lo(h) - bf16_lo(l), p1 - bf16_hi(h) - bf16_hi(l));
+                    }
                 }
                 l_run += psum;
             };
@@ -445,6 +452,10 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
                         const bf16x8 vf = __builtin_bit_cast(bf16x8, v8);
                         acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, acc_o[db], 0, 0, 0);
                         acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf_lo, acc_o[db], 0, 0, 0);
+                        if constexpr (EX) {
+                            const u32x4 pt = u32x4{third[4 * kstep], third[4 * kstep + 1], third[4 * kstep + 2], third[4 * kstep + 3]};
+                            acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pt), acc_o[db], 0, 0, 0);
+                        }
                     }
                 }
             };
@@ -457,8 +468,9 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
             scores(sa, sb);
             settle(sa, sb);
             weights(sa, pa, pa_lo);
+            if constexpr (EX) accumulate(0, pa, pa_lo);
             weights(sb, pb_, pb_lo);
-            accumulate(0, pa, pa_lo);
+            if constexpr (!EX) accumulate(0, pa, pa_lo);
             accumulate(32, pb_, pb_lo);
         }
         if constexpr (FP4) {

@@ -80,7 +80,8 @@ def bounds(case, bf16_out, scale=None):
       scores   a sum of d exact products in 32 bits: each addition is off by 2^-24 of a partial sum, which is at most |q| |k|
                (`smax` with the scale); sqrt(d) of them add up at random, eight standard deviations of that; the
                exponential and the scale's own product add 2^-22 of the exponent
-      weights  split into two bfloat16 halves: half a step of the second, 2^-17 of the weight
+      weights  split into two bfloat16 parts for a bfloat16 output, half a step of the second being 2^-17 of the weight, and
+               into three for an fp32 one, 2^-26
       output   a mean of values of at most `vmax` with those weights, whose relative errors count twice (in the sum above
                and the sum below); half a step, 2^-8 of it, where it is stored in bfloat16
       norm     the errors of the weights do not add up coherently: one standard deviation of them, twice
@@ -91,6 +92,7 @@ def bounds(case, bf16_out, scale=None):
     smax = abs(case.scale if scale is None else scale) * (np.linalg.norm(case.q.reshape(-1, d).astype(np.float64), axis=-1).max() *
                                                           np.linalg.norm(keys, axis=-1).max())
     score = (8 * d ** 0.5 * 2.0 ** -24 + 2.0 ** -22) * smax
-    out = vmax * (2 * score + 2.0 ** -16)
-    norm = 2 * (2.0 ** -17 + d ** 0.5 * 2.0 ** -24 * smax)
+    weight = 2.0 ** (-17 if bf16_out else -26)
+    out = vmax * (2 * score + 2 * weight + 2.0 ** -22)          # (and the sums of a few thousand weights in 32 bits)
+    norm = 2 * (weight + d ** 0.5 * 2.0 ** -24 * smax)
     return out + (vmax * 2.0 ** -8 if bf16_out else 0.0), score + 2.0 ** -16, norm + (2.0 ** -8 if bf16_out else 0.0)
