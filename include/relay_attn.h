@@ -474,7 +474,7 @@ ra_status relay_attn_system_fill(const ra_params *p,
  * bf16 cache.  A value is its magnitude times its block's power of two; attention takes it as that, exactly (in
  * bf16 products with fp32 sums), so the result is that of the bf16 entry points on the same values.  The shared
  * system cache stays bf16: it is read once per batch, and stored once.
- *   block_size is a power of two from 8 on here (RA_ERR_UNSUPPORTED below).  Positions at or beyond a request's length
+ *   block_size is a power of two from 8 to 2^24 here (RA_ERR_UNSUPPORTED otherwise).  Positions at or beyond a request's length
  * that share its last block may be read, whatever they hold, and count for nothing; block-table slots behind the ones in use
  * are never followed.
  * relay_attn_fp4_cache_bytes: host arithmetic; the bytes of one (block, kv head) and of one whole cache (k or v) for
@@ -485,9 +485,11 @@ ra_status relay_attn_fp4_cache_bytes(const ra_params *p, size_t *block_bytes_out
 /*
  * relay_attn_cache_append for the 4-bit cache: rounds the new keys/values into it.  For each 32 channels of a row, a
  * being the largest magnitude, the power of two is 2^(floor(log2 a) - 2), twice that where a >= 1.75 * 2^floor(log2 a), and within
- * 2^-127 .. 2^125; values round to the nearest multiple there (halves to the even code) and saturate at 6.  So no finite value below
- * 2^127 is off by more than half a step of the grid, 1/6 of itself or 1/14 of a.  The format has no infinity and no NaN: both count
- * as the largest magnitude and are stored as 6 * 2^125, so that a row with one in it spoils every result that sees it and no other.
+ * 2^-127 .. 2^125; values round to the nearest of the grid (halves to the even code) and saturate at 6.  So a value below 7 * 2^125 is
+ * off by at most half a step of the grid at its place (N(0, 1) values: 11 % of their norm).  The format has no infinity and no NaN:
+ * both count as the largest magnitude and are stored as 6 * 2^125, which spoils every result that sees it and, unlike a
+ * NaN, no other.
+ *   num_blocks     has to be filled in: places are checked against it
  *   slot_map       NULL: new token j of request i goes to the position that relay_attn_cache_append gives it.  Otherwise
  *                  device, [total_q]: the place of each token, physical block * block_size + offset in it
  *                  (relay_attn_update_tables writes such a map); a token whose entry is not in 0 .. num_blocks *
@@ -508,7 +510,8 @@ ra_status relay_attn_cache_append_fp4(const ra_params *p,
  * The way back: the values of rows of the 4-bit cache as bf16 (exact), named as in relay_attn_cache_append_fp4, into
  * k_out / v_out, [total_q] tokens x Hkv x head_dim addressed by the strides given.  With the strides of a system cache it
  * turns a request's context (m_i = context_lens[i] "new" tokens) into a shared system prompt.  Rows whose slot is out of
- * range are left as they are.
+ * range are left as they are.  Rows of the output may not overlap (RA_ERR_INVALID_ARG): either the heads of a token are
+ * in front of the next token, or the tokens of a head in front of the next head.
  */
 ra_status relay_attn_cache_read_fp4(const ra_params *p,
                                     void *k_out, void *v_out,
@@ -521,6 +524,9 @@ ra_status relay_attn_cache_read_fp4(const ra_params *p,
 
 /*
  * relay_attn_decode and relay_attn_prefill over a 4-bit context cache: arguments, result, workspace and errors as there.
+ * The weights of the softmax enter the products as two bfloat16 parts (2^-17 of a weight is lost) for a bf16 output and as three
+ * for an fp32 one.  A prompt phase whose requests bring few new tokens each (max_q_len * Hq / Hkv up to 32) over long contexts
+ * streams the contexts as a decode step does; like every cut of the work this changes the result by rounding at most.
  */
 ra_status relay_attn_decode_fp4(const ra_params *p,
                                 const void *q,

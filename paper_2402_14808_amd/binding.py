@@ -432,8 +432,8 @@ def fp4_cache_shape(num_blocks, num_kv_heads, block_size, head_dim):
 def _fp4_rows(fn, where, params, k, v, cu_seqlens_q, total_q, k_cache, v_cache, block_tables, context_lens, slot_map):
     strides = k.stride()
     assert v.stride() == strides and strides[2] == 1
-    st = fn(ctypes.byref(params), k.data_ptr(), v.data_ptr(), strides[0], strides[1], _ptr(cu_seqlens_q), total_q,
-            _ptr(slot_map), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(block_tables), _ptr(context_lens), _stream())
+    st = fn(ctypes.byref(params), k.data_ptr(), v.data_ptr(), strides[0], strides[1], _ptr(cu_seqlens_q),
+            int(total_q), _ptr(slot_map), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(block_tables), _ptr(context_lens), _stream())
     if st != RA_OK:
         raise RelayAttnError(st, where)
 

@@ -9,7 +9,7 @@
 
 using ra::aligned16;
 using ra::check_params;
-using ra::kFp4LeastBlock;
+using ra::fp4_block_size;
 
 namespace {
 
@@ -19,16 +19,19 @@ ra_status fp4_rows(const ra_params *p, void *k, void *v, int64_t stride_token, i
                    const int32_t *block_tables, const int32_t *context_lens, void *hip_stream, bool read) {
     const ra_status st = check_params(p, total_q);
     if (st != RA_OK) return st;
-    if (p->block_size < kFp4LeastBlock) return RA_ERR_UNSUPPORTED;
+    if (!fp4_block_size(p->block_size)) return RA_ERR_UNSUPPORTED;
     if (stride_token < 0 || stride_head < 0 || stride_token % 8 || stride_head % 8) return RA_ERR_INVALID_ARG;
     if (!slot_map && !cu_seqlens_q && total_q != p->batch) return RA_ERR_INVALID_ARG;
     if (total_q == 0) return RA_OK;
     if (!k || !v || !k_cache || !v_cache) return RA_ERR_INVALID_ARG;
+    if (p->num_blocks < 1) return RA_ERR_INVALID_ARG;        // (no place would be in range)
     if (!slot_map && (p->batch < 1 || !block_tables || !context_lens)) return RA_ERR_INVALID_ARG;
     if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache)) return RA_ERR_INVALID_ARG;
     if (stride_head < p->head_dim && p->num_kv_heads > 1) return RA_ERR_INVALID_ARG;
-    // (rows that are written may not overlap)
-    if (read && total_q > 1 && stride_token < p->head_dim) return RA_ERR_INVALID_ARG;
+    // Rows that are written may not overlap: tokens behind all heads of a token, or heads behind all tokens of a head.
+    if (read && total_q > 1 && stride_token < (p->num_kv_heads - 1) * stride_head + p->head_dim &&
+        (stride_token < p->head_dim || stride_head < (total_q - 1) * stride_token + p->head_dim))
+        return RA_ERR_INVALID_ARG;
     ra::Fp4RowsArgs a{};
     a.k_rows = static_cast<uint16_t *>(k);
     a.v_rows = static_cast<uint16_t *>(v);
@@ -60,7 +63,7 @@ ra_status relay_attn_fp4_cache_bytes(const ra_params *p, size_t *block_bytes_out
     if (!p || !block_bytes_out || !bytes_out) return RA_ERR_INVALID_ARG;
     if (p->num_kv_heads < 1 || p->num_blocks < 0 || p->block_size < 1 || (p->block_size & (p->block_size - 1)) != 0)
         return RA_ERR_INVALID_ARG;
-    if ((p->head_dim != 64 && p->head_dim != 128) || p->block_size < kFp4LeastBlock) return RA_ERR_UNSUPPORTED;
+    if ((p->head_dim != 64 && p->head_dim != 128) || !fp4_block_size(p->block_size)) return RA_ERR_UNSUPPORTED;
     *block_bytes_out = (size_t)p->block_size * (p->head_dim / 2 + p->head_dim / 32);
     *bytes_out = *block_bytes_out * (size_t)p->num_kv_heads * (size_t)p->num_blocks;
     return RA_OK;

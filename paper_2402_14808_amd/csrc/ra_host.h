@@ -8,7 +8,9 @@
 
 namespace ra {
 
-constexpr int kFp4LeastBlock = 8;     // the 4-bit kernels take eight positions of a block at a time
+// Block sizes of a 4-bit cache: its kernels take eight positions of a block at a time, and count bytes of a block in 31 bits.
+constexpr int kFp4LeastBlock = 8, kFp4MostBlock = 1 << 24;
+inline bool fp4_block_size(int32_t block_size) { return block_size >= kFp4LeastBlock && block_size <= kFp4MostBlock; }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -20,7 +20,6 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 using ra::aligned16;
 using ra::check_params;
-using ra::kFp4LeastBlock;
 
 namespace {
 
@@ -685,7 +684,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
     ra_status st = check_params(p, total_q);
     if (st != RA_OK) return st;
     const bool fp4 = fp4_calls != nullptr;
-    if (fp4 && p->block_size < kFp4LeastBlock) return RA_ERR_UNSUPPORTED;
+    if (fp4 && !ra::fp4_block_size(p->block_size)) return RA_ERR_UNSUPPORTED;
     if (naive && p->sys_len != 0) return RA_ERR_INVALID_ARG;
     if (append) {
         if (append->stride_token < 0 || append->stride_head < 0 || append->stride_token % 8 ||

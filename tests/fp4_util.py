@@ -85,6 +85,9 @@ def bounds(case, bf16_out, scale=None):
       output   a mean of values of at most `vmax` with those weights, whose relative errors count twice (in the sum above
                and the sum below); half a step, 2^-8 of it, where it is stored in bfloat16
       norm     the errors of the weights do not add up coherently: one standard deviation of them, twice
+      sums     what is left at a scale of zero, where all scores are equal: each of n additions of a sum over n positions is off
+               by at most 2^-24 of a partial sum, at random sqrt(n) 2^-24 of the sum; then the reciprocal, its product, the
+               weight in the merge and the stored fp32 result are rounded once each, 4 * 2^-24
     """
     d = case.cfg.head_dim
     keys = np.concatenate([np.nan_to_num(case.k_sys).reshape(-1, d), case.k_cache.reshape(-1, d)]).astype(np.float64)
@@ -93,6 +96,7 @@ def bounds(case, bf16_out, scale=None):
                                                           np.linalg.norm(keys, axis=-1).max())
     score = (8 * d ** 0.5 * 2.0 ** -24 + 2.0 ** -22) * smax
     weight = 2.0 ** (-17 if bf16_out else -26)
-    out = vmax * (2 * score + 2 * weight + 2.0 ** -22)          # (and the sums of a few thousand weights in 32 bits)
-    norm = 2 * (weight + d ** 0.5 * 2.0 ** -24 * smax)
+    sums = ((case.cfg.sys_len + int(case.context_lens.max())) ** 0.5 + 4) * 2.0 ** -24
+    out = vmax * (2 * score + 2 * weight + sums)
+    norm = 2 * (weight + d ** 0.5 * 2.0 ** -24 * smax) + sums
     return out + (vmax * 2.0 ** -8 if bf16_out else 0.0), score + 2.0 ** -16, norm + (2.0 ** -8 if bf16_out else 0.0)

@@ -33,8 +33,15 @@ def test_rows_in_and_out_refuse(name):
 
 
 def test_read_refuses_rows_on_top_of_each_other():
-    assert _rows("relay_attn_cache_read_fp4", _params(), st=0) == BAD
-    assert _rows("relay_attn_cache_read_fp4", _params(), st=64) == BAD
+    for st, sh in ((0, 128), (64, 128), (128, 128), (248, 128), (128, 8 * 128 + 120)):      # 9 tokens of 2 heads of 128
+        assert _rows("relay_attn_cache_read_fp4", _params(), st=st, sh=sh) == BAD, (st, sh)
+
+
+def test_rows_want_to_know_how_many_blocks_there_are():
+    for name in ("relay_attn_cache_append_fp4", "relay_attn_cache_read_fp4"):
+        assert _rows(name, _params(num_blocks=0)) == BAD
+        assert _rows(name, _params(num_blocks=0), slots=FAKE) == BAD
+        assert _rows(name, _params(block_size=1 << 25, max_blocks_per_seq=4)) == NOT_HERE
 
 
 def _attend(p, prefill, q=FAKE, ks=FAKE, vs=FAKE, kc=FAKE, vc=FAKE, bt=FAKE, cl=FAKE, out=FAKE, ws=FAKE, ws_bytes=1 << 40,
@@ -55,6 +62,7 @@ def test_attention_refuses_what_the_bf16_calls_refuse_and_small_blocks(prefill):
     assert _attend(p, prefill, ws_bytes=0) == binding.RA_ERR_WORKSPACE_TOO_SMALL
     for bs in (1, 2, 4):
         assert _attend(_params(block_size=bs, max_blocks_per_seq=128), prefill) == NOT_HERE
+    assert _attend(_params(block_size=1 << 25, max_blocks_per_seq=4), prefill) == NOT_HERE
     assert _attend(_params(reserved0=7), prefill) == BAD
     if prefill:
         assert _attend(p, True, cu=None) == BAD and _attend(p, True, most=1) == BAD and _attend(p, True, n=-1) == BAD

@@ -213,7 +213,11 @@ DECODE = [
 @pytest.mark.parametrize("fp32_out", [True, False], ids=["fp32", "bf16"])
 def test_decode_matches_oracle(cfg, fp32_out):
     _say("%s" % (cfg,))
-    Fp4Case(W.make_case(cfg, 911)).check(fp32_out=fp32_out)
+    fc = Fp4Case(W.make_case(cfg, 911))
+    fc.check(fp32_out=fp32_out)
+    fc.check(fp32_out=fp32_out, ctx_part_tokens=128)             # two launches whatever the size
+    if cfg.sys_len:
+        fc.check(fp32_out=fp32_out, sys_chunk_tokens=64)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -245,9 +249,9 @@ def test_decode_of_a_strided_query_and_extreme_scales():
     wide = torch.zeros((case.cfg.batch, 20, 136), dtype=torch.bfloat16, device=DEV)
     wide[:, 3:15, :128] = fc.q
     fc.check(q=wide[:, 3:15, :128])
-    for scale in (-0.05, 0.0, 3.0):
-        _say("scale %g" % scale)
-        out, lse = _run_scaled(fc, scale)
+    for scale, part in [(s, part) for s in (-0.05, 0.0, 3.0) for part in (0, 128)]:       # one launch, and two
+        _say("scale %g, part %d" % (scale, part))
+        out, lse = _run_scaled(fc, scale, part)
         c = fc.case
         want, wlse = oracle.decode_attention(c.q, c.k_sys, c.v_sys, c.k_cache, c.v_cache, c.block_tables, c.context_lens,
                                              scale)[:2]
@@ -256,13 +260,15 @@ def test_decode_of_a_strided_query_and_extreme_scales():
         assert np.linalg.norm(out - want) <= rel * np.linalg.norm(want)
 
 
-def _run_scaled(fc, scale):
+def _run_scaled(fc, scale, part):
     c = fc.case
-    out, lse = torch.empty(fc.q.shape, device=DEV), torch.empty(fc.q.shape[:2], device=DEV)
-    p = ra.make_params(fc.q, out, fc.k_sys, fc.k, fc.tables, batch=c.cfg.batch, softmax_scale=scale)
+    wide = torch.full((fc.q.shape[0], fc.q.shape[1] + 2, fc.q.shape[2] + 8), 7.0, device=DEV)   # rows of a wider output
+    out, lse = wide[:, 1:-1, :-8], torch.empty(fc.q.shape[:2], device=DEV)
+    p = ra.make_params(fc.q, out, fc.k_sys, fc.k, fc.tables, batch=c.cfg.batch, softmax_scale=scale, ctx_part_tokens=part)
     ws = torch.empty(ra.relay_attn_workspace_bytes(p, c.cfg.batch), dtype=torch.uint8, device=DEV)
     ra.relay_attn_decode_fp4(p, fc.q, fc.k_sys, fc.v_sys, fc.k, fc.v, fc.tables, fc.lens, out, lse, ws)
     torch.cuda.synchronize()
+    assert (wide[:, 0] == 7).all() and (wide[:, -1] == 7).all() and (wide[:, :, -8:] == 7).all()
     return out.cpu().numpy(), lse.cpu().numpy()
 
 
@@ -372,6 +378,33 @@ def test_a_cache_beyond_four_gigabytes():
     torch.cuda.synchronize()
     want, _ = W.logical_context(fc.case, 0)
     assert np.array_equal(rows.float().cpu().numpy(), want)
+
+
+def test_a_context_becomes_a_system_prompt():
+    """The whole context of a request, read out into a system cache in the recommended layout, is seen by the others of its
+    batch as if they had it in front of their own."""
+    cfg = _cfg(batch=3, sys_len=0, ctx_lo=77, ctx_hi=200, num_q_heads=4, num_kv_heads=4)
+    fc = Fp4Case(W.make_case(cfg, 991))
+    n, hkv, d = int(fc.case.context_lens[0]), 4, 128
+    k_sys, v_sys = (ra.system_cache_view(torch.full((ra.relay_attn_system_cache_layout(n, hkv, d)[2] // 2,), float("nan"),
+                                                    dtype=torch.bfloat16, device=DEV), n, hkv, d) for _ in range(2))
+    p = ra.make_params(fc.q, fc.q, None, fc.k, fc.tables, batch=1, softmax_scale=1.0)
+    ra.relay_attn_cache_read_fp4(p, k_sys, v_sys, _i32([0, n]), n, fc.k, fc.v, fc.tables, fc.lens)
+    torch.cuda.synchronize()
+    k, v = W.logical_context(fc.case, 0)
+    assert np.array_equal(k_sys.float().cpu().numpy(), k) and np.array_equal(v_sys.float().cpu().numpy(), v)
+    fc.k_sys, fc.v_sys = k_sys, v_sys
+    fc.case = replace(fc.case, cfg=replace(cfg, sys_len=n), k_sys=k, v_sys=v)
+    fc.check()
+
+
+def test_a_block_that_holds_a_whole_context():
+    fc = Fp4Case(W.make_case(_cfg(batch=3, block_size=4096, ctx_lo=1500, ctx_hi=3900, num_q_heads=4, num_kv_heads=2), 993))
+    fc.check()
+    fc.check(ctx_part_tokens=256)
+    few = Fp4Case(W.make_case(_cfg(batch=2, block_size=2048, ctx_lo=1500, ctx_hi=1700, num_q_heads=4, num_kv_heads=2, q_lo=3,
+                                   q_hi=9, head_dim=64), 994, prefill=True, extra_context=True))
+    few.check(prefill=True)
 
 
 def test_block_placement_and_stream_do_not_change_a_bit():
