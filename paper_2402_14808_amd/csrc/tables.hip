@@ -7,14 +7,17 @@
 // after the first) and then does its share of the requests, or of the tokens.  Nothing that one workgroup writes is
 // read by another: taken blocks come from the stack below `held` or from table columns that only shrinking requests have,
 // and the stack is written between `held` and its new height, which is empty when any of the blocks below are taken.
-// Bound: the launch and a chain of four trips to memory, not bytes.
+// Bound: the launch and a chain of trips to memory, not bytes: lengths, then the block of a place, which for one that was just
+// given back is a search through the sums and a trip to its table.  4.0 us for 64 requests of a token each; 15 us for 1500 of which
+// some end, some give back and the others bring up to 700 tokens (6 of them without any change of a table: summing 1500 lengths).
 #include "ra_device.h"
 #include "ra_kernels.h"
 
 namespace ra {
 
 namespace {
-constexpr int kSlots = 4;        // consecutive tokens per thread
+template <int T>
+constexpr int kTableSlots = T == 1024 ? 4 : 1;
 
 struct Step {                    // what one request asks for
     int had, want, need, back, old_len, new_len;
@@ -47,6 +50,9 @@ struct Sums {
 template <int T>
 __global__ __launch_bounds__(T) void update_tables_kernel(const TableArgs a, const int request_groups) {
     constexpr int WAVES = T / kWave;
+    // Consecutive tokens per thread: with many requests the search for a token's is worth sharing; with few each token wants a
+    // thread of its own (64 requests of a token each: 4.0 us, 5.0 with four).
+    constexpr int kSlots = kTableSlots<T>;
     __shared__ Sums<T> sm;
     __shared__ int sm_wave[2][WAVES];
     __shared__ int64_t sm_wave_tokens[WAVES];
@@ -61,8 +67,10 @@ __global__ __launch_bounds__(T) void update_tables_kernel(const TableArgs a, con
     const int r0 = min(tid * per, a.batch), r1 = min(r0 + per, a.batch);
     int need = 0, back = 0;
     int64_t tokens = 0;
+    Step mine{};                                  // the first of the run: with up to T requests, the only one
+    if (r0 < r1) mine = step_of(a, r0);
     for (int r = r0; r < r1; ++r) {
-        const Step s = step_of(a, r);
+        const Step s = r == r0 ? mine : step_of(a, r);
         need += s.need, back += s.back, tokens += tokens_of(s);
     }
     int need_to = need, back_to = back;
@@ -88,7 +96,7 @@ __global__ __launch_bounds__(T) void update_tables_kernel(const TableArgs a, con
     auto served = [&](const Step &s, int through) { return s.fits && (s.need == 0 || through <= top); };
     int taken = 0, unserved = 0;
     for (int r = r0, through = need_to - need; r < r1; ++r) {
-        const Step s = step_of(a, r);
+        const Step s = r == r0 ? mine : step_of(a, r);
         through += s.need;
         if (!served(s, through)) ++unserved;
         else if (s.need > 0) taken = through;
@@ -157,7 +165,7 @@ __global__ __launch_bounds__(T) void update_tables_kernel(const TableArgs a, con
         return;
     }
 
-    // ---- slots of the new tokens, kSlots consecutive ones per thread: one search, then on from request to request
+    // ---- slots of the new tokens: one search per thread, then on from request to request
     const int64_t first = ((int64_t)((int)blockIdx.x - request_groups) * T + tid) * kSlots;
     if (first >= a.n_slots) return;
     int32_t slot[kSlots];
@@ -192,18 +200,21 @@ __global__ __launch_bounds__(T) void update_tables_kernel(const TableArgs a, con
             if (id >= 0 && id < a.num_blocks) slot[k] = (id << bsl) + (pos & ((1 << bsl) - 1));
         }
     }
-    if (first + kSlots <= a.n_slots && (reinterpret_cast<uintptr_t>(a.slot_map) & 15u) == 0) {
-        *reinterpret_cast<u32x4 *>(a.slot_map + first) = u32x4{(uint32_t)slot[0], (uint32_t)slot[1], (uint32_t)slot[2], (uint32_t)slot[3]};
-    } else {
-#pragma unroll
-        for (int k = 0; k < kSlots; ++k)
-            if (first + k < a.n_slots) a.slot_map[first + k] = slot[k];
+    if constexpr (kSlots == 4) {
+        if (first + kSlots <= a.n_slots && (reinterpret_cast<uintptr_t>(a.slot_map) & 15u) == 0) {
+            *reinterpret_cast<u32x4 *>(a.slot_map + first) =
+                u32x4{(uint32_t)slot[0], (uint32_t)slot[1], (uint32_t)slot[2], (uint32_t)slot[3]};
+            return;
+        }
     }
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k)
+        if (first + k < a.n_slots) a.slot_map[first + k] = slot[k];
 }
 
 template <int T>
 static void launch_tables(const TableArgs &a, hipStream_t stream) {
-    constexpr int WAVES = T / kWave;
+    constexpr int WAVES = T / kWave, kSlots = kTableSlots<T>;
     int request_groups = (a.batch + WAVES - 1) / WAVES;
     if (request_groups > 256) request_groups = 256;
     if (request_groups < 1) request_groups = 1;            // (an empty batch hands its pool on)
@@ -213,8 +224,9 @@ static void launch_tables(const TableArgs &a, hipStream_t stream) {
 }
 
 hipError_t launch_update_tables(const TableArgs &a, hipStream_t stream) {
-    // A thread goes through its run of requests one after the other, and a token through the run that it is in: with
-    // 1500 requests of up to 700 new tokens, 256 threads (runs of six) took 26 us.  Few requests start sooner in a small workgroup.
+    // A thread goes through its run of requests one after the other, and a token through the run that it is in: 1500 requests of
+    // up to 700 new tokens took 26 us with 256 threads (runs of six) and take 15 with 1024.  Few requests start sooner in a small
+    // workgroup.
     if (a.batch > 512) launch_tables<1024>(a, stream);
     else launch_tables<256>(a, stream);
     return hipGetLastError();
