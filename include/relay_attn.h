@@ -487,8 +487,8 @@ ra_status relay_attn_fp4_cache_bytes(const ra_params *p, size_t *block_bytes_out
  * being the largest magnitude, the power of two is 2^(floor(log2 a) - 2), twice that where a >= 1.75 * 2^floor(log2 a), and within
  * 2^-127 .. 2^125; values round to the nearest of the grid (halves to the even code) and saturate at 6.  So a value below 7 * 2^125 is
  * off by at most half a step of the grid at its place (N(0, 1) values: 11 % of their norm).  The format has no infinity and no NaN:
- * both count as the largest magnitude and are stored as 6 * 2^125, which spoils every result that sees it and, unlike a
- * NaN, no other.
+ * both count as the largest magnitude and are stored as 6 * 2^125 with their sign.  Results that see such a position
+ * are of that size, no number, or without it where its score is far below the others; unlike a NaN's, they are no others.
  *   num_blocks     has to be filled in: places are checked against it
  *   slot_map       NULL: new token j of request i goes to the position that relay_attn_cache_append gives it.  Otherwise
  *                  device, [total_q]: the place of each token, physical block * block_size + offset in it

@@ -342,7 +342,8 @@ __device__ __forceinline__ void fp4_attend(const TileArgs &a, const int req, con
                 *reinterpret_cast<f32x4 *>(to + n) =
                     f32x4{acc[c][n][r] * inv, acc[c][n + 1][r] * inv, acc[c][n + 2][r] * inv, acc[c][n + 3][r] * inv};
         }
-        if (h == 0) a.part_lse[prow] = l > 0.f ? msc[c] + log2f(l) : -INFINITY;
+        // (a sum that is no number, of a query or a score that is none, must not look like an empty partial)
+        if (h == 0) a.part_lse[prow] = l == 0.f ? -INFINITY : msc[c] + log2f(l);
     }
 }
 

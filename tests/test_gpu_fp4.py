@@ -356,6 +356,59 @@ def test_an_infinity_spoils_the_results_that_see_it_and_no_other():
     assert not np.array_equal(results[0][0][25:40], results[1][0][25:40])
 
 
+@pytest.mark.parametrize("kw", [{}, dict(ctx_part_tokens=128)])
+@pytest.mark.parametrize("prefill", [False, True])
+def test_a_query_that_is_no_number_gives_none_and_leaves_the_others(prefill, kw):
+    case = W.make_case(_cfg(batch=4, ctx_lo=40, ctx_hi=300, q_lo=2, q_hi=9), 955, prefill=prefill, extra_context=prefill)
+    fc = Fp4Case(case)
+    bad = 2
+    q = fc.q.clone()
+    q[bad, 5, 17] = float("nan")
+    clean, lse = fc.run(prefill, **kw)
+    got, _ = fc.run(prefill, q=q, **kw)
+    rest = np.ones(got.shape[:2], dtype=bool)
+    rest[bad, 5] = False
+    assert np.isnan(got[bad, 5]).all()
+    tol, _, _ = F.bounds(fc.case, False)                        # (running maxima are moved by groups of rows)
+    assert np.abs(got[rest] - clean[rest]).max() <= 2 * tol
+
+
+def test_a_step_whose_pool_runs_dry():
+    """Requests that are not served keep their length, their new tokens have no slots, and the others are served in full."""
+    rng = np.random.Generator(np.random.PCG64(957))
+    B, hq, hkv, d, bs, s, blocks = 5, 8, 2, 64, 8, 30, 12
+    counts = [17, 30, 5, 40, 8]                                  # 3 + 4 + 1 + 5 blocks of 12: the fourth is not served, nor the last
+    served = [True, True, True, False, False]
+    new = lambda *shape: W.bf16_round(rng.standard_normal(shape, dtype=np.float32))  # noqa: E731
+    k_sys, v_sys, n = new(s, hkv, d), new(s, hkv, d), sum(counts)
+    q, kn, vn = new(n, hq, d), new(n, hkv, d), new(n, hkv, d)
+    k, v = (torch.full(ra.fp4_cache_shape(blocks, hkv, bs, d), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(2))
+    tables = torch.full((B, 6), W.POISON_BLOCK, dtype=torch.int32, device=DEV)
+    free, pool, pool_out = _i32(rng.permutation(blocks)), _i32([blocks, 0]), _i32([0, 0])
+    held, cu, slots = _i32([-1] * B), _i32([-1] * (B + 1)), _i32([-7] * n)
+    ra.relay_attn_update_tables(ra.make_table_params(tables, num_blocks=blocks, block_size=bs), _i32([0] * B), _i32(counts), pool,
+                                pool_out, free, tables, held, cu, slots)
+    out, lse = torch.full((n, hq, d), float("nan"), device=DEV), torch.empty((n, hq), device=DEV)
+    ks, vs = _bf16(k_sys), _bf16(v_sys)
+    p = ra.make_params(_bf16(q), out, ks, k, tables, batch=B, softmax_scale=d ** -0.5)
+    ws = torch.full((ra.relay_attn_workspace_bytes(p, n),), 0xFF, dtype=torch.uint8, device=DEV)
+    ra.relay_attn_cache_append_fp4(p, _bf16(kn), _bf16(vn), None, n, k, v, None, None, slot_map=slots)
+    ra.relay_attn_prefill_fp4(p, _bf16(q), cu, n, max(counts), ks, vs, k, v, tables, held, out, lse, ws)
+    torch.cuda.synchronize()
+    assert held.tolist() == [c if ok else 0 for c, ok in zip(counts, served)] and pool_out.tolist() == [4, 2]
+    at = np.cumsum([0] + counts)
+    assert cu.tolist() == at.tolist()
+    rows = [[F.values(*F.round_rows(x[at[i]:at[i + 1]])).astype(np.float32) for i in range(3)] for x in (kn, vn)]
+    cfg = _cfg(batch=3, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, block_size=bs, sys_len=s)
+    m = int(at[3])
+    case = W.from_dense(cfg, q[:m], k_sys, v_sys, *rows, cu_seqlens_q=at[:4].astype(np.int32), poison_tails=False)
+    want, _, _ = oracle.prefill_attention(q[:m], case.cu_seqlens_q, k_sys, v_sys, case.k_cache, case.v_cache, case.block_tables,
+                                          case.context_lens, case.scale)
+    got = out.cpu().numpy()
+    assert np.abs(got[:m] - want).max() <= F.bounds(case, False)[0]
+    assert (slots[m:] == -1).all() and np.isfinite(got[m:]).all()   # the others see the system prompt alone
+
+
 def test_a_cache_beyond_four_gigabytes():
     """Blocks at the far end of a cache whose byte offsets pass 32 bits."""
     d, bs, hkv, hq = 128, 64, 8, 8
