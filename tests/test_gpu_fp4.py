@@ -77,7 +77,7 @@ class Fp4Case:
         tol, ltol, rel = F.bounds(self.case, not fp32_out)
         empty = np.isneginf(wlse)
         assert np.array_equal(np.isneginf(lse), empty)
-        err, lerr = np.abs(got - want).max(), np.abs(lse - wlse)[~empty].max(initial=0.0)
+        err, lerr = np.abs(got - want).max(), np.abs(lse[~empty] - wlse[~empty]).max(initial=0.0)
         off = np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-30)
         _say("max-abs err %.3e of %.3e, lse err %.3e of %.3e, norm %.3e of %.3e" % (err, tol, lerr, ltol, off, rel))
         assert np.isfinite(got).all() and err <= tol and lerr <= ltol and off <= rel
