@@ -17,6 +17,7 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.4028234663852886e38f;
 constexpr int kWave = 64;
 constexpr int kThreads = 256;  // every kernel here runs 4 wavefronts per workgroup
 

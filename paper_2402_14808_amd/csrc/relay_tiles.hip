@@ -237,7 +237,9 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
     for (int db = 0; db < T::DBLK; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc_o[db][r] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    // (the lowest number and not minus infinity, which scores can be that overflow: their difference would be no number, and
+    // they have to count for nothing)
+    float m_run = kLowest, l_run = 0.f;
 
     // V^T operand geometry for ds_read_b64_tr_b16: inside each block of 16 lanes, lane r
     // addresses 4 consecutive head_dim elements of row K0 + r/4 starting at D0 + 4*(r%4);
@@ -285,7 +287,7 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
         for (int r = 4; r < 16; r += 4)
             mx = fmaxf(mx, fmaxf(fmaxf(s[r], s[r + 1]), fmaxf(s[r + 2], s[r + 3])));
         mx = max_with_other_half(mx);
-        const float m_new = fmaxf(m_run, mx);     // finite: every processed tile has a valid key
+        const float m_new = fmaxf(m_run, mx);
         if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {   // some column's maximum moved
             const float corr = fast_exp2(m_run - m_new);
             l_run *= corr;
@@ -368,7 +370,7 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
                                      acc_o[db][4 * r4 + 2] * inv, acc_o[db][4 * r4 + 3] * inv};
                     *reinterpret_cast<f32x4 *>(dst + db * 32 + 8 * r4 + 4 * hf) = v;
                 }
-            if (hf == 0) a.part_lse[prow] = l_run > 0.f ? m_run + log2f(l_run) : -INFINITY;
+            if (hf == 0) a.part_lse[prow] = l_run == 0.f ? -INFINITY : m_run + log2f(l_run);   // (see fp4_attend.h)
         }
         return;
     }
@@ -400,11 +402,10 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
         float Mr = sm_m[0][row];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) Mr = fmaxf(Mr, sm_m[w][row]);
-        const float m_use = finite_or_zero(Mr);
         float L = 0.f, f[kWaves];
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            f[w] = fast_exp2(sm_m[w][row] - m_use);
+            f[w] = fast_exp2(sm_m[w][row] - Mr);
             L = fmaf(sm_l[w][row], f[w], L);
         }
         const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -423,7 +424,7 @@ __device__ __forceinline__ void attend(const TileArgs &a, const Item &it, const 
             }
             *reinterpret_cast<f32x4 *>(dst + e) = sum * inv;
         }
-        if (seg == 0) a.part_lse[prow] = L > 0.f ? Mr + log2f(L) : -INFINITY;
+        if (seg == 0) a.part_lse[prow] = L == 0.f ? -INFINITY : Mr + log2f(L);       // (see fp4_attend.h)
     }
 }
 

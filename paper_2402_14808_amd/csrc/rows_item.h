@@ -568,8 +568,7 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
                                  acc_o[db][4 * r4 + 2] * inv, acc_o[db][4 * r4 + 3] * inv};
                 *reinterpret_cast<f32x4 *>(dst + db * 32 + 8 * r4 + 4 * hf) = v;
             }
-        const bool empty = FP4 ? l_run == 0.f : !(l_run > 0.f);      // (see fp4_attend.h)
-        if (hf == 0) a.part_lse[prow] = empty ? -INFINITY : msc + log2f(l_run);
+        if (hf == 0) a.part_lse[prow] = l_run == 0.f ? -INFINITY : msc + log2f(l_run);      // (see fp4_attend.h)
     }
 }
 
