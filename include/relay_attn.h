@@ -37,6 +37,9 @@
  *     out, k_sys, v_sys and the caches is contiguous; every row start must be
  *     16-byte aligned (base pointers 16-byte aligned, strides multiples of 8
  *     elements).
+ *   - A not-a-number in a query, or in a key that a row sees, makes the row's output and lse_out not-a-numbers, and
+ *     so does a score that overflows to plus infinity; no other row changes.  lse_out is minus infinity only where
+ *     a row sees no position, or none whose score does not overflow to that.  (All but paged_attn_decode_naive.)
  *   - Errors are returned as ra_status, never thrown.  All argument checks
  *     happen before the first HIP call, so they behave the same on a machine
  *     without a GPU.  Contents of device arrays (block-table entries, context

@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kDirectThreads, 4) void decode_direct_kernel(
     const int64_t oo = (int64_t)token * a.o_stride_token + (int64_t)h * a.o_stride_head + d;
     if (a.out_is_fp32) static_cast<float *>(a.out)[oo] = acc;
     else static_cast<uint16_t *>(a.out)[oo] = (uint16_t)f32_to_bf16_bits(acc);
-    if (d == 0 && a.lse_out) a.lse_out[(int64_t)token * a.Hq + h] = W > 0.f ? (m_use + log2f(W)) * kLn2 : -INFINITY;
+    if (d == 0 && a.lse_out) a.lse_out[(int64_t)token * a.Hq + h] = W == 0.f ? -INFINITY : (m_use + log2f(W)) * kLn2;
 }
 
 }  // namespace ra

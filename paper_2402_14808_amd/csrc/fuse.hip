@@ -152,7 +152,8 @@ __global__ __launch_bounds__(kThreads) void fuse_kernel(const FuseArgs a) {
         u32x2 w2 = {pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
         *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + oo) = w2;
     }
-    if (e == 0 && a.lse_out) a.lse_out[row] = W > 0.f ? (finite_or_zero(M) + log2f(W)) * kLn2 : -INFINITY;
+    // (minus infinity means that the row saw no position: a sum that is no number must not look like that)
+    if (e == 0 && a.lse_out) a.lse_out[row] = W == 0.f ? -INFINITY : (finite_or_zero(M) + log2f(W)) * kLn2;
 }
 
 // Cache append: a workgroup moves the rows of `tpw` consecutive tokens (K and V, all kv heads), a

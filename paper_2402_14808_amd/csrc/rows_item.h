@@ -548,7 +548,7 @@ __device__ __forceinline__ void rows_item(const RowsArgs &a, const int block, un
                     }
                 }
             if (hf == 0 && a.lse_out)
-                a.lse_out[(int64_t)token * a.Hq + hq] = l_run > 0.f ? (msc + log2f(l_run)) * kLn2 : -INFINITY;
+                a.lse_out[(int64_t)token * a.Hq + hq] = l_run == 0.f ? -INFINITY : (msc + log2f(l_run)) * kLn2;
         }
         return;
     }

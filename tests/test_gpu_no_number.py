@@ -1,5 +1,5 @@
-"""Results that are no number, in every form a call can run in: a row whose query or whose keys hold one gives none, and no other
-row changes."""
+"""Results that are no number, in every form a call can run in: a row whose query or whose keys hold one gives none, in its
+output and in its log-sum-exp, and no other row changes."""
 import sys
 from dataclasses import replace
 
@@ -64,9 +64,9 @@ class Call:
 
 
 def _compare(call, got, want, bad, case, both_off=1):
-    """Rows `bad` are no numbers, the others are those of `want`."""
+    """Rows `bad` are no numbers in output and log-sum-exp, the others are those of `want`."""
     tol, ltol = call.tolerances(case)
-    assert np.isnan(got[0][bad]).all()
+    assert np.isnan(got[0][bad]).all() and np.isnan(got[1][bad]).all()
     assert np.abs(got[0][~bad] - want[0][~bad]).max() <= both_off * tol
     empty = np.isneginf(want[1])
     assert np.array_equal(np.isneginf(got[1])[~bad], empty[~bad])
