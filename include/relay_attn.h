@@ -562,7 +562,7 @@ ra_status relay_attn_prefill_fp4(const ra_params *p,
  *   pool_out       [2], another array than pool_in: [0] = the new height, [1] = number of requests not served
  *   context_lens   [batch], another array than the lengths: new_lens[i], or old_lens[i] where request i is not served
  *   cu_seqlens_q   nullable; [batch + 1]: running sums of max(0, new_lens[i] - old_lens[i]), served or not, so that they fit
- *                  the packed new tokens of the caller
+ *                  the packed new tokens of the caller (see below)
  *   slot_map       [num_slots] (may be NULL if that is 0): for each packed new token physical block * block_size + offset;
  *                  -1 for tokens of requests that are not served, and behind the last token
  * Blocks that come back go on top of the stack in (request, column) order; then requests take theirs from the top in that
@@ -570,6 +570,14 @@ ra_status relay_attn_prefill_fp4(const ra_params *p,
  * ask for; one that needs none always is, and one whose new length exceeds max_blocks_per_seq * block_size never.  The same call on the same
  * inputs has the same results, and may be repeated on its own outputs (the inputs that it updates are
  * still good for it).
+ *   Where pool_out[1] is above zero, cu_seqlens_q and context_lens disagree: a request that is not served keeps its length, and its
+ * new tokens still count.  Calls that find rows by the two (relay_attn_cache_append; relay_attn_cache_append_fp4 and
+ * relay_attn_cache_read_fp4 without a slot_map; relay_attn_decode_append by context_lens alone) would take the LAST
+ * CACHED positions of such a request for its new tokens' and write over them.  So append by slot_map, which leaves
+ * them out, or call again with the context_lens of this call as new_lens (and another array for context_lens), everything else as
+ * it is: tables, stack and its height stay as they are, every request is served, and cu_seqlens_q counts the tokens of
+ * those that grow only, for the caller to pack.  Attention over the arrays of the first call is safe; the rows of a request that is not
+ * served have no meaning.  (A decode step without cu_seqlens_q has to leave such requests out of its batch.)
  * Uses p->batch, block_size, num_blocks and max_blocks_per_seq only.  block_tables entries and stack entries are
  * taken on trust as in every call (an id out of range gets its tokens the slot -1).  RA_ERR_UNSUPPORTED where num_blocks *
  * block_size, or batch * max_blocks_per_seq + num_blocks, exceeds 31 bits.

@@ -481,7 +481,9 @@ def make_table_params(block_tables, *, num_blocks, block_size) -> RAParams:
 
 def relay_attn_update_tables(params, old_lens, new_lens, pool_in, pool_out, free_blocks, block_tables, context_lens,
                              cu_seqlens_q, slot_map):
-    """int32 device tensors; cu_seqlens_q and slot_map may be None."""
+    """int32 device tensors; cu_seqlens_q and slot_map may be None.  A step that leaves requests unserved (pool_out[1] > 0)
+    appends by slot_map, or calls again with context_lens as new_lens and appends by what that gives: the calls that place rows
+    by lengths would write over the last cached rows of a request that is not served."""
     st = load().relay_attn_update_tables(
         ctypes.byref(params), old_lens.data_ptr(), new_lens.data_ptr(), pool_in.data_ptr(), pool_out.data_ptr(),
         free_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(cu_seqlens_q), _ptr(slot_map),
