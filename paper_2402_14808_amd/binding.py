@@ -223,8 +223,16 @@ def _check(status, where):
         raise RelayAttnError(status, where)
 
 
+def _check_caches(where, width, k_cache, v_cache):
+    """Refuses a 4-bit cache (bytes) where a bfloat16 one is addressed, which is about four times as long, and the other way
+    round; width: bytes of an element."""
+    if (k_cache is not None and k_cache.element_size() != width) or (v_cache is not None and v_cache.element_size() != width):
+        raise RelayAttnError(RA_ERR_INVALID_ARG, where)
+
+
 def relay_attn_decode(params, q, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens,
                       out, lse_out, workspace):
+    _check_caches("relay_attn_decode", 2, k_cache, v_cache)
     st = load().relay_attn_decode(
         ctypes.byref(params), _ptr(q), _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache),
         _ptr(block_tables), _ptr(context_lens), _ptr(out), _ptr(lse_out), _ptr(workspace),
@@ -235,6 +243,7 @@ def relay_attn_decode(params, q, k_sys, v_sys, k_cache, v_cache, block_tables, c
 def relay_attn_decode_append(params, q, k_new, v_new, k_sys, v_sys, k_cache, v_cache, block_tables,
                              context_lens, out, lse_out, workspace):
     """k_new / v_new: [batch, Hkv, d] tensors (any token / head strides, d contiguous)."""
+    _check_caches("relay_attn_decode_append", 2, k_cache, v_cache)
     assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
     st = load().relay_attn_decode_append(
         ctypes.byref(params), _ptr(q), _ptr(k_new), _ptr(v_new), int(k_new.stride(0)),
@@ -247,6 +256,7 @@ def relay_attn_decode_append(params, q, k_new, v_new, k_sys, v_sys, k_cache, v_c
 def relay_attn_debug_timeline(params, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache,
                               block_tables, context_lens, out, lse_out, workspace, timeline):
     """timeline: int64 / uint64 device tensor of 2 * n values (n wavefronts recorded)."""
+    _check_caches("relay_attn_debug_timeline", 2, k_cache, v_cache)
     st = load().relay_attn_debug_timeline(
         ctypes.byref(params), _ptr(q), _ptr(cu_seqlens_q), int(total_q), int(max_q_len), _ptr(k_sys),
         _ptr(v_sys), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(context_lens), _ptr(out),
@@ -257,6 +267,7 @@ def relay_attn_debug_timeline(params, q, cu_seqlens_q, total_q, max_q_len, k_sys
 
 def relay_attn_decode_static(params, q, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens,
                              out, lse_out):
+    _check_caches("relay_attn_decode_static", 2, k_cache, v_cache)
     st = load().relay_attn_decode_static(
         ctypes.byref(params), _ptr(q), _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache),
         _ptr(block_tables), _ptr(context_lens), _ptr(out), _ptr(lse_out), _stream())
@@ -279,6 +290,7 @@ def relay_attn_static_scratch_bytes() -> int:
 
 def relay_attn_debug_decode_phases(params, phases, q, k_sys, v_sys, k_cache, v_cache, block_tables,
                                    context_lens, out, lse_out, workspace):
+    _check_caches("relay_attn_debug_decode_phases", 2, k_cache, v_cache)
     st = load().relay_attn_debug_decode_phases(
         ctypes.byref(params), int(phases), _ptr(q), _ptr(k_sys), _ptr(v_sys), _ptr(k_cache),
         _ptr(v_cache), _ptr(block_tables), _ptr(context_lens), _ptr(out), _ptr(lse_out),
@@ -288,6 +300,7 @@ def relay_attn_debug_decode_phases(params, phases, q, k_sys, v_sys, k_cache, v_c
 
 def relay_attn_prefill(params, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache,
                        v_cache, block_tables, context_lens, out, lse_out, workspace):
+    _check_caches("relay_attn_prefill", 2, k_cache, v_cache)
     st = load().relay_attn_prefill(
         ctypes.byref(params), _ptr(q), _ptr(cu_seqlens_q), int(total_q), int(max_q_len),
         _ptr(k_sys), _ptr(v_sys), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
@@ -299,6 +312,7 @@ def relay_attn_prefill(params, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys
 def relay_attn_prefill_multi(params, groups, group_tokens, q, cu_seqlens_q, total_q, max_q_len, k_cache,
                              v_cache, block_tables, context_lens, out, lse_out, workspace):
     """groups: as for make_prefixes; group_tokens: new tokens of each group (host ints)."""
+    _check_caches("relay_attn_prefill_multi", 2, k_cache, v_cache)
     arr = make_prefixes(groups) if isinstance(groups, (list, tuple)) else groups
     toks = (ctypes.c_int32 * len(arr))(*[int(x) for x in group_tokens])
     st = load().relay_attn_prefill_multi(
@@ -311,6 +325,7 @@ def relay_attn_prefill_multi(params, groups, group_tokens, q, cu_seqlens_q, tota
 
 def paged_attn_decode_naive(params, q, k_cache, v_cache, block_tables, context_lens, out,
                             lse_out, workspace):
+    _check_caches("paged_attn_decode_naive", 2, k_cache, v_cache)
     st = load().paged_attn_decode_naive(
         ctypes.byref(params), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_tables),
         _ptr(context_lens), _ptr(out), _ptr(lse_out), _ptr(workspace),
@@ -321,6 +336,7 @@ def paged_attn_decode_naive(params, q, k_cache, v_cache, block_tables, context_l
 def relay_attn_cache_append(params, k_new, v_new, cu_seqlens_q, total_q, k_cache, v_cache,
                             block_tables, context_lens):
     """k_new / v_new: [total_q, Hkv, d] tensors (any token / head strides, d contiguous)."""
+    _check_caches("relay_attn_cache_append", 2, k_cache, v_cache)
     assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
     st = load().relay_attn_cache_append(
         ctypes.byref(params), _ptr(k_new), _ptr(v_new), int(k_new.stride(0)), int(k_new.stride(1)),
@@ -345,6 +361,7 @@ def make_prefixes(groups):
 def relay_attn_decode_multi(params, groups, q, k_cache, v_cache, block_tables, context_lens, out,
                             lse_out, workspace):
     """groups: a list as for make_prefixes, or the array it returned."""
+    _check_caches("relay_attn_decode_multi", 2, k_cache, v_cache)
     arr = make_prefixes(groups) if isinstance(groups, (list, tuple)) else groups
     st = load().relay_attn_decode_multi(
         ctypes.byref(params), len(arr), arr, _ptr(q), _ptr(k_cache), _ptr(v_cache),
@@ -368,6 +385,7 @@ def relay_attn_decode_grouped(params, prefixes, sys_id, request_order, q, k_cach
                               block_tables, context_lens, out, lse_out, workspace):
     """prefixes: list of (k_sys, v_sys, num_requests) per application (k_sys None for an empty
     prefix); sys_id / request_order: int32 device tensors [batch]."""
+    _check_caches("relay_attn_decode_grouped", 2, k_cache, v_cache)
     arr = make_prefixes([(k, v, 0, n) for k, v, n in prefixes])
     st = load().relay_attn_decode_grouped(
         ctypes.byref(params), len(arr), arr, _ptr(sys_id), _ptr(request_order), _ptr(q),
@@ -430,6 +448,7 @@ def fp4_cache_shape(num_blocks, num_kv_heads, block_size, head_dim):
 
 # (Addresses are taken in place and strides once: a small call costs the host more than the GPU.)
 def _fp4_rows(fn, where, params, k, v, cu_seqlens_q, total_q, k_cache, v_cache, block_tables, context_lens, slot_map):
+    _check_caches(where, 1, k_cache, v_cache)
     strides = k.stride()
     assert v.stride() == strides and strides[2] == 1
     st = fn(ctypes.byref(params), k.data_ptr(), v.data_ptr(), strides[0], strides[1], _ptr(cu_seqlens_q),
@@ -455,6 +474,7 @@ def relay_attn_cache_read_fp4(params, k_out, v_out, cu_seqlens_q, total_q, k_cac
 
 
 def relay_attn_decode_fp4(params, q, k_sys, v_sys, k_cache, v_cache, block_tables, context_lens, out, lse_out, workspace):
+    _check_caches("relay_attn_decode_fp4", 1, k_cache, v_cache)
     st = load().relay_attn_decode_fp4(
         ctypes.byref(params), q.data_ptr(), _ptr(k_sys), _ptr(v_sys), k_cache.data_ptr(), v_cache.data_ptr(),
         block_tables.data_ptr(), context_lens.data_ptr(), out.data_ptr(), _ptr(lse_out), workspace.data_ptr(),
@@ -464,6 +484,7 @@ def relay_attn_decode_fp4(params, q, k_sys, v_sys, k_cache, v_cache, block_table
 
 def relay_attn_prefill_fp4(params, q, cu_seqlens_q, total_q, max_q_len, k_sys, v_sys, k_cache, v_cache, block_tables,
                            context_lens, out, lse_out, workspace):
+    _check_caches("relay_attn_prefill_fp4", 1, k_cache, v_cache)
     st = load().relay_attn_prefill_fp4(
         ctypes.byref(params), q.data_ptr(), _ptr(cu_seqlens_q), int(total_q), int(max_q_len),
         _ptr(k_sys), _ptr(v_sys), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(),

@@ -33,7 +33,8 @@
 //     high and a low bf16 part so that no 2^-9 rounding of the weights reaches the output).
 // Reduction order depends only on the logical position of a key, never on the physical block,
 // so any block placement of the same cache gives bit-identical results.  Rows past the end of
-// an item are never loaded (their lanes re-load the item's last row and the scores are masked);
+// an item over bfloat16 rows are never loaded (their lanes re-load the item's last row and the scores are masked; a span of
+// a 4-bit cache loads the rest of its last block, see fp4_attend.h);
 // block-table slots past the last used block may be read but are never dereferenced.
 #include "fp4_attend.h"
 #include "ra_device.h"
