@@ -527,10 +527,15 @@ ra_status relay_attn_cache_read_fp4(const ra_params *p,
 
 /*
  * relay_attn_decode and relay_attn_prefill over a 4-bit context cache: arguments, result, workspace and errors as there.
+ * relay_attn_workspace_bytes_fp4 is the size for a call that takes the form it likes best; it is above
+ * relay_attn_workspace_bytes for prompt phases of few new tokens only, and with that many bytes they take fewer partials, or
+ * the other form.
  * The weights of the softmax enter the products as two bfloat16 parts (2^-17 of a weight is lost) for a bf16 output and as three
  * for an fp32 one.  A prompt phase whose requests bring few new tokens each (max_q_len * Hq / Hkv up to 32) over long contexts
  * streams the contexts as a decode step does; like every cut of the work this changes the result by rounding at most.
  */
+size_t relay_attn_workspace_bytes_fp4(const ra_params *p, int32_t total_q);
+
 ra_status relay_attn_decode_fp4(const ra_params *p,
                                 const void *q,
                                 const void *k_sys, const void *v_sys,

@@ -27,7 +27,7 @@ EXPORTED = ("relay_attn_workspace_bytes", "relay_attn_decode_plan", "relay_attn_
             "relay_attn_decode_grouped", "relay_attn_group_requests", "relay_attn_prefill_multi",
             "relay_attn_debug_stream_probe", "relay_attn_debug_launch_probe",
             "relay_attn_fp4_cache_bytes", "relay_attn_cache_append_fp4", "relay_attn_cache_read_fp4",
-            "relay_attn_decode_fp4", "relay_attn_prefill_fp4", "relay_attn_update_tables",
+            "relay_attn_decode_fp4", "relay_attn_prefill_fp4", "relay_attn_workspace_bytes_fp4", "relay_attn_update_tables",
             "relay_attn_status_string", "relay_attn_abi_version")
 
 
@@ -44,6 +44,7 @@ class RAParams(ctypes.Structure):
         ("out_is_fp32", ctypes.c_int32), ("sys_chunk_tokens", ctypes.c_int32),
         ("ctx_part_tokens", ctypes.c_int32), ("reserved0", ctypes.c_int32),
     ]
+    fp4_cache = False        # made from a 4-bit cache (make_params): what its workspace is sized for; not part of the C structure
 
 
 class RAPrefix(ctypes.Structure):
@@ -89,6 +90,8 @@ def load() -> ctypes.CDLL:
     P, V, I32, SZ = ctypes.POINTER(RAParams), ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
     lib.relay_attn_workspace_bytes.restype = SZ
     lib.relay_attn_workspace_bytes.argtypes = [P, I32]
+    lib.relay_attn_workspace_bytes_fp4.restype = SZ
+    lib.relay_attn_workspace_bytes_fp4.argtypes = [P, I32]
     lib.relay_attn_decode.restype = ctypes.c_int
     lib.relay_attn_decode.argtypes = [P, V, V, V, V, V, V, V, V, V, V, SZ, V]
     lib.relay_attn_decode_append.restype = ctypes.c_int
@@ -191,6 +194,7 @@ def make_params(q, out, k_sys, k_cache, block_tables, *, batch, softmax_scale,
     if k_cache.dtype == torch.uint8:                   # head_dim * 17 / 32 bytes a position
         assert k_cache.dim() == 3 and k_cache.shape[2] * 32 % (17 * p.head_dim) == 0
         p.block_size = int(k_cache.shape[2]) * 32 // (17 * p.head_dim)
+        p.fp4_cache = True
     p.num_blocks = int(k_cache.shape[0])
     p.max_blocks_per_seq = int(block_tables.shape[1])
     p.max_context_len = int(max_context_len)
@@ -215,7 +219,14 @@ def relay_attn_decode_plan(params: RAParams) -> RADecodePlan:
 
 
 def relay_attn_workspace_bytes(params: RAParams, total_q: int) -> int:
+    """(Of parameters that make_params made from a 4-bit cache: relay_attn_workspace_bytes_fp4.)"""
+    if params.fp4_cache:
+        return relay_attn_workspace_bytes_fp4(params, total_q)
     return int(load().relay_attn_workspace_bytes(ctypes.byref(params), int(total_q)))
+
+
+def relay_attn_workspace_bytes_fp4(params: RAParams, total_q: int) -> int:
+    return int(load().relay_attn_workspace_bytes_fp4(ctypes.byref(params), int(total_q)))
 
 
 def _check(status, where):

@@ -1120,8 +1120,14 @@ size_t relay_attn_workspace_bytes(const ra_params *p, int32_t total_q) {
         const Plan bound = make_plan(p, total_q, kRelayDecode, 1, 0, rows_sys, SIZE_MAX, {}, DecodeWay{true});
         if (!bound.unsupported && bound.bytes > most) most = bound.bytes;
     }
-    // (and a prompt phase of few new tokens over a 4-bit cache)
-    if (total_q > p->batch && p->batch > 0 && (int64_t)total_q * (p->num_q_heads / p->num_kv_heads) <= (int64_t)kFewRows * p->batch) {
+    return most;
+}
+
+size_t relay_attn_workspace_bytes_fp4(const ra_params *p, int32_t total_q) {
+    size_t most = relay_attn_workspace_bytes(p, total_q);
+    // a prompt phase of few new tokens, which streams the contexts
+    if (most > 0 && total_q > p->batch && p->batch > 0 &&
+        (int64_t)total_q * (p->num_q_heads / p->num_kv_heads) <= (int64_t)kFewRows * p->batch) {
         DecodeWay way;
         way.contexts = p->batch;
         const Plan few = make_plan(p, total_q, kRelayDecode, 1, 0, true, SIZE_MAX, {}, way);
