@@ -532,7 +532,9 @@ ra_status relay_attn_cache_read_fp4(const ra_params *p,
  * the other form.
  * The weights of the softmax enter the products as two bfloat16 parts (2^-17 of a weight is lost) for a bf16 output and as three
  * for an fp32 one.  A prompt phase whose requests bring few new tokens each (max_q_len * Hq / Hkv up to 32) over long contexts
- * streams the contexts as a decode step does; like every cut of the work this changes the result by rounding at most.
+ * streams the contexts as a decode step does; like every cut of the work this changes the result by rounding at most.  How long
+ * contexts are is taken from max_context_len and from what num_blocks can hold: fill in the first where the cache is a server's
+ * whole memory.
  */
 size_t relay_attn_workspace_bytes_fp4(const ra_params *p, int32_t total_q);
 

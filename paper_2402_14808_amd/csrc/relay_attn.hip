@@ -739,12 +739,21 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
     // 40 heads, 6 .. 7 tokens behind 525 .. 782, 54.7 -> 32.9 us; one of 52, 4 .. 8 tokens, no context, 9.6 -> 13.3).
     bool few = fp4 && cu_seqlens_q && total_q > 0 && max_q_len <= kFewRows / (p->num_q_heads / p->num_kv_heads) &&
                p->sys_chunk_tokens == 0 && p->ctx_part_tokens == 0;
+    bool known = true;
     if (few) {
         const double most = p->max_context_len > 0 ? p->max_context_len : (double)p->max_blocks_per_seq * p->block_size;
         double held = (double)p->num_blocks * p->block_size;
-        if (held < total_q) held = p->batch * most;                  // (was not filled in)
+        const bool filled = held >= total_q;                         // (num_blocks was filled in)
+        if (!filled) held = p->batch * most;
         const double mean = held / p->batch < most ? held / p->batch : most;
         few = mean >= 1024 || p->batch * p->num_kv_heads * mean / 32 >= 1000;
+        // Both are upper bounds.  Without max_context_len, and with a cache that would hold the batch twice over at the block
+        // tables' capacity, neither says anything; the spans that a wavefront takes at least, which this form plans for that
+        // capacity, are then what short contexts wait for.  Of 99 drawn calls of that kind the 84 with spans of up to eight tiles
+        // take 0.96 of the many-rows time (0.41 .. 2.5) and the others 1.31 (0.42 .. 7.1: 16 requests of 40 heads, 8 .. 27
+        // tokens behind 32 .. 137 under 7600, 24.5 -> 173 us).  (141 drawn calls with pools of 1 .. 8 times their contents and bounds of 1 .. 40
+        // times their contexts that do say something: 0.83, 0.38 .. 2.1.)
+        known = p->max_context_len > 0 || (filled && held <= 2 * p->batch * most);
     }
     if (few) {
         DecodeWay way;
@@ -753,7 +762,7 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         // (a workspace of another call's size: as many slots as it holds, or the other form)
         if (!stream.unsupported && stream.bytes > workspace_bytes)
             stream = make_plan(p, total_q, kRelayDecode, 1, 0, true, workspace_bytes, {}, way);
-        few = !stream.unsupported && stream.bytes <= workspace_bytes;
+        few = !stream.unsupported && stream.bytes <= workspace_bytes && (known || stream.ctx_t_floor <= 8);
         if (few) pl = stream;
     }
     for (size_t budget : {SIZE_MAX, workspace_bytes}) {
