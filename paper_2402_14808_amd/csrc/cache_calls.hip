@@ -19,7 +19,7 @@ ra_status fp4_rows(const ra_params *p, void *k, void *v, int64_t stride_token, i
                    const int32_t *block_tables, const int32_t *context_lens, void *hip_stream, bool read) {
     const ra_status st = check_params(p, total_q);
     if (st != RA_OK) return st;
-    if (!fp4_block_size(p->block_size)) return RA_ERR_UNSUPPORTED;
+    if (!fp4_block_size(p->block_size) || !ra::token_pieces_fit(p)) return RA_ERR_UNSUPPORTED;
     if (stride_token < 0 || stride_head < 0 || stride_token % 8 || stride_head % 8) return RA_ERR_INVALID_ARG;
     if (!slot_map && !cu_seqlens_q && total_q != p->batch) return RA_ERR_INVALID_ARG;
     if (total_q == 0) return RA_OK;

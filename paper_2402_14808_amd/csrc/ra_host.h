@@ -12,6 +12,9 @@ namespace ra {
 constexpr int kFp4LeastBlock = 8, kFp4MostBlock = 1 << 24;
 inline bool fp4_block_size(int32_t block_size) { return block_size >= kFp4LeastBlock && block_size <= kFp4MostBlock; }
 
+// Rows that a call moves: a workgroup counts the 16-byte pieces of a token (of all kv heads) in 31 bits, with room for a round.
+inline bool token_pieces_fit(const ra_params *p) { return (int64_t)p->num_kv_heads * (p->head_dim / 8) <= 1 << 30; }
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 inline ra_status check_params(const ra_params *p, int32_t total_q) {

@@ -1399,6 +1399,7 @@ ra_status relay_attn_cache_append(const ra_params *p, const void *k_new, const v
                                   const int32_t *context_lens, void *hip_stream) {
     ra_status st = check_params(p, total_q);
     if (st != RA_OK) return st;
+    if (!ra::token_pieces_fit(p)) return RA_ERR_UNSUPPORTED;
     if (new_stride_token < 0 || new_stride_head < 0 || new_stride_token % 8 || new_stride_head % 8)
         return RA_ERR_INVALID_ARG;
     if (!cu_seqlens_q && total_q != p->batch) return RA_ERR_INVALID_ARG;
