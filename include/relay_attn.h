@@ -421,7 +421,8 @@ ra_status paged_attn_decode_naive(const ra_params *p,
  * context_lens[i] already counts the new tokens (the convention of every entry point here):
  * new token j of the m_i tokens of request i is written to context position
  * context_lens[i] - m_i + j, i.e. into block block_tables[i][pos / block_size] at offset
- * pos % block_size.  Only k_cache / v_cache are written; nothing is allocated.
+ * pos % block_size.  Tokens behind cu_seqlens_q[batch] (a batch padded to total_q) and ones whose position is below 0 are left out.
+ * Only k_cache / v_cache are written; nothing is allocated.
  */
 ra_status relay_attn_cache_append(const ra_params *p,
                                   const void *k_new, const void *v_new,
@@ -511,7 +512,7 @@ ra_status relay_attn_cache_append_fp4(const ra_params *p,
 
 /*
  * The way back: the values of rows of the 4-bit cache as bf16 (exact), named as in relay_attn_cache_append_fp4, into
- * k_out / v_out, [total_q] tokens x Hkv x head_dim addressed by the strides given.  With the strides of a system cache it
+ * k_out / v_out, [total_q] tokens x Hkv x head_dim addressed by the strides given (tokens that an append leaves out are left as they are).  With the strides of a system cache it
  * turns a request's context (m_i = context_lens[i] "new" tokens) into a shared system prompt.  Rows whose slot is out of
  * range are left as they are.  Rows of the output may not overlap (RA_ERR_INVALID_ARG): either the heads of a token are
  * in front of the next token, or the tokens of a head in front of the next head.

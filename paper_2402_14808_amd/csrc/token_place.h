@@ -5,7 +5,7 @@
 
 namespace ra {
 
-// Lane l of a whole wavefront: request and context position of token token0 + l, for the first `tpw` lanes.  Without
+// Lane l of a whole wavefront: request and context position (below 0: none) of token token0 + l, for the first `tpw` lanes.  Without
 // cu_seqlens_q token i is request i, and the position is left to the caller (0 here).
 // The lanes hold the bounds and lengths of 64 requests at a time, so that a token's place is one trip
 // to its block id away once they are here (searched first and asked for then, the lengths were a
@@ -28,14 +28,15 @@ __device__ __forceinline__ void place_of_token(const int32_t *cu_seqlens_q, cons
                 const int ended = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= token0 + t));
                 if (lane == t) owner = ended;
             }
-            // (a token that no request owns goes to the last one)
+            // (a token behind the last request's, in a padded batch, has no place: counted on from that request it lay
+            // beyond its context, in a block whose table slot is not in use)
             const bool last = base + kWave >= batch;
             const int from = min(owner, min(batch - base, kWave) - 1);
             const int f = __shfl(first, from), e = __shfl(end, from), l = __shfl(len, from);
             if (!found && (owner < kWave || last)) {
                 found = true;
                 req = base + from;
-                pos = l - (e - f) + (token - f);
+                pos = token < e ? l - (e - f) + (token - f) : -1;
             }
         }
     }
