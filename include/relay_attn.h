@@ -482,7 +482,7 @@ ra_status relay_attn_system_fill(const ra_params *p,
  * that share its last block may be read, whatever they hold, and count for nothing; block-table slots behind the ones in use
  * are never followed.
  * relay_attn_fp4_cache_bytes: host arithmetic; the bytes of one (block, kv head) and of one whole cache (k or v) for
- * p->num_blocks, num_kv_heads, block_size and head_dim.
+ * p->num_blocks, num_kv_heads, block_size and head_dim (RA_ERR_UNSUPPORTED where that passes 64 bits).
  */
 ra_status relay_attn_fp4_cache_bytes(const ra_params *p, size_t *block_bytes_out, size_t *bytes_out);
 

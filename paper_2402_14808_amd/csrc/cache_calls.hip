@@ -65,7 +65,9 @@ ra_status relay_attn_fp4_cache_bytes(const ra_params *p, size_t *block_bytes_out
         return RA_ERR_INVALID_ARG;
     if ((p->head_dim != 64 && p->head_dim != 128) || !fp4_block_size(p->block_size)) return RA_ERR_UNSUPPORTED;
     *block_bytes_out = (size_t)p->block_size * (p->head_dim / 2 + p->head_dim / 32);
-    *bytes_out = *block_bytes_out * (size_t)p->num_kv_heads * (size_t)p->num_blocks;
+    // (a size that is cut off to 64 bits would be taken for a small one)
+    const size_t rows = (size_t)p->num_kv_heads * (size_t)p->num_blocks;       // below 2^62
+    if (__builtin_mul_overflow(*block_bytes_out, rows, bytes_out)) return RA_ERR_UNSUPPORTED;
     return RA_OK;
 }
 
