@@ -577,7 +577,7 @@ ra_status relay_attn_prefill_fp4(const ra_params *p,
  * order.  A request that needs blocks is served as long as the stack holds what it and all requests in front of it
  * ask for; one that needs none always is, and one whose new length exceeds max_blocks_per_seq * block_size never.  The same call on the same
  * inputs has the same results, and may be repeated on its own outputs (the inputs that it updates are
- * still good for it).
+ * still good for it).  Arrays that are written may not lie on each other or on ones that are read (RA_ERR_INVALID_ARG).
  *   Where pool_out[1] is above zero, cu_seqlens_q and context_lens disagree: a request that is not served keeps its length, and its
  * new tokens still count.  Calls that find rows by the two (relay_attn_cache_append; relay_attn_cache_append_fp4 and
  * relay_attn_cache_read_fp4 without a slot_map; relay_attn_decode_append by context_lens alone) would take the LAST

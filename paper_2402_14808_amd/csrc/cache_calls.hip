@@ -53,6 +53,15 @@ ra_status fp4_rows(const ra_params *p, void *k, void *v, int64_t stride_token, i
                                                                                                        : RA_ERR_HIP;
 }
 
+struct Range {                                            // of 32-bit numbers; null: none
+    const int32_t *first;
+    int64_t n;
+    bool meets(const Range &o) const {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(first), b = reinterpret_cast<uintptr_t>(o.first);
+        return first && o.first && n > 0 && o.n > 0 && a < b + 4 * (uintptr_t)o.n && b < a + 4 * (uintptr_t)n;
+    }
+};
+
 constexpr ra::Fp4Calls kFp4Calls{ra::launch_decode_direct_fp4};
 
 }  // namespace
@@ -128,6 +137,14 @@ ra_status relay_attn_update_tables(const ra_params *p, const int32_t *old_lens, 
     if ((int64_t)p->batch * p->max_blocks_per_seq + p->num_blocks > INT32_MAX ||
         (int64_t)p->num_blocks * p->block_size > INT32_MAX)
         return RA_ERR_UNSUPPORTED;
+    // Every workgroup reads all lengths and the pool's height while others write: nothing written may lie on anything else.
+    const Range arrays[] = {{pool_out, 2},    {context_lens, p->batch}, {cu_seqlens_q, (int64_t)p->batch + 1}, {slot_map, num_slots},
+                            {free_blocks, p->num_blocks}, {block_tables, (int64_t)p->batch * p->max_blocks_per_seq},
+                            {pool_in, 2},     {old_lens, p->batch},     {new_lens, p->batch}};
+    constexpr int kWritten = 6;
+    for (int i = 0; i < kWritten; ++i)
+        for (int j = i + 1; j < (int)(sizeof(arrays) / sizeof(arrays[0])); ++j)
+            if (arrays[i].meets(arrays[j])) return RA_ERR_INVALID_ARG;
     ra::TableArgs a{};
     a.old_lens = old_lens;
     a.new_lens = new_lens;
