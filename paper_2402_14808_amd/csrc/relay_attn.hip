@@ -742,18 +742,19 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
     bool known = true;
     if (few) {
         const double most = p->max_context_len > 0 ? p->max_context_len : (double)p->max_blocks_per_seq * p->block_size;
+        const double batch = p->batch;
         double held = (double)p->num_blocks * p->block_size;
         const bool filled = held >= total_q;                         // (num_blocks was filled in)
-        if (!filled) held = p->batch * most;
-        const double mean = held / p->batch < most ? held / p->batch : most;
-        few = mean >= 1024 || p->batch * p->num_kv_heads * mean / 32 >= 1000;
+        if (!filled) held = batch * most;
+        const double mean = held / batch < most ? held / batch : most;
+        few = mean >= 1024 || batch * p->num_kv_heads * mean / 32 >= 1000;
         // Both are upper bounds.  Without max_context_len, and with a cache that would hold the batch twice over at the block
         // tables' capacity, neither says anything; the spans that a wavefront takes at least, which this form plans for that
         // capacity, are then what short contexts wait for.  Of 99 drawn calls of that kind the 84 with spans of up to eight tiles
         // take 0.96 of the many-rows time (0.41 .. 2.5) and the others 1.31 (0.42 .. 7.1: 16 requests of 40 heads, 8 .. 27
         // tokens behind 32 .. 137 under 7600, 24.5 -> 173 us).  (141 drawn calls with pools of 1 .. 8 times their contents and bounds of 1 .. 40
         // times their contexts that do say something: 0.83, 0.38 .. 2.1.)
-        known = p->max_context_len > 0 || (filled && held <= 2 * p->batch * most);
+        known = p->max_context_len > 0 || (filled && held <= 2 * batch * most);
     }
     if (few) {
         DecodeWay way;
@@ -1008,7 +1009,9 @@ ra_status run(const ra_params *p, const void *q, const int32_t *cu_seqlens_q, in
         // workgroups 256 .. 256 + n_sys - 1 sit next to a system workgroup.
         // (A system tile holds a unit up as long as about three tiles of a 4-bit context, which are 0.27 of its bytes: 64
         // requests of 40 heads, 300 .. 2500 behind 1024, 108.9 us counted as one, 105.6 as two, 101.7 as three, 106 as five.  With
-        // two groups of rows a context tile takes as long: 32 requests of 2 .. 8 tokens, 26.0 us counted as one, 30.9 as three.)
+        // two groups of rows a context tile takes as long: 32 requests of 2 .. 8 tokens, 26.0 us counted as one, 30.9 as three.
+        // With many-rows system items, whose steps the wavefronts of a workgroup share, 40 drawn steps of 33 .. 253 requests take
+        // 0.991 of the time counted as one when counted as two, 0.988 as three (0.88 .. 1.15) and 1.063 as five.)
         const int ctx_per_sys_tile = fp4 && !prefill ? 3 : 1;
         if (pl.paired && items + pl.ctx_wgs == kWorkgroupSlots && items <= kWorkgroupSlots / 2) {
             t.ctx_light_begin = (kWorkgroupSlots / 2 - items) * 4;
