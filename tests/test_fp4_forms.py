@@ -7,6 +7,7 @@ import pytest
 import fp4_launches as L
 import launch_record as R
 import test_gpu_fp4 as T
+import test_gpu_fp4_graph as G
 import test_gpu_no_number as N
 import workloads as W
 from test_fp4_workspace import shape
@@ -50,6 +51,13 @@ def test_the_forms_that_are_tested_for_no_numbers_are_those_named(form, want):
     cfg, prompts, kw = N.FORMS[form]
     for seed in (1201, 1202, 1203):
         assert _form(_launches(cfg, seed, prompts, **kw)) == want
+
+
+@pytest.mark.parametrize("name,want", zip(G.SHAPES, ["few", "few", "whole", "many rows"]))
+def test_the_forms_that_are_captured_are_those_named(name, want):
+    cfg, counts, longest = G.SHAPES[name]
+    width = -(-longest // cfg.block_size)
+    assert _form(_of(cfg, [longest], np.cumsum([0] + counts), cfg.batch * width + 3, width=width)) == want
 
 
 def test_both_forms_of_few_new_tokens_are_tested():
